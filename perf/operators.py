@@ -1,0 +1,411 @@
+"""Serving operators as measurable cases: the tables of a paged cache, the cache's rows in 4 bits, and attention over them.
+
+The cache holds keys and values as E2M1 codes (1 sign, 2 exponent bits, 1 mantissa bit: 0, .5, 1, 1.5, 2, 3, 4, 6), two to a
+byte, the even element in the low half, with one scale 2^(byte - 127) for 32 consecutive elements of a head.  Per page:
+codes [heads, page, dim / 2], scales [heads, dim / 32, page].
+
+Inputs are synthetic and made on the GPU from the seed: keys and values are normal with channels of different strength, as
+projections of activations are; pages lie in random order, and what no request owns holds rows of others.  The lengths of
+a case are the same for every seed, in another order, so that every seed does the same work.
+"""
+import math
+import random
+
+import torch
+
+own = False
+DEV = "cuda"
+TORCH = {"bf16": torch.bfloat16, "f32": torch.float32}
+SIZE = {"bf16": 2, "f32": 4}
+BLOCK = 32       # elements of a scale
+
+
+# ---- cases -----------------------------------------------------------------------------------------------
+def _tables(name, requests, past, new, page, empty=0):
+    """past, new: shortest and longest of a batch, spread evenly over their logarithm; empty: requests with neither."""
+    return {"name": name, "kind": "tables", "requests": requests, "past_lo": past[0], "past_hi": past[1], "new_lo": new[0],
+            "new_hi": new[1], "page": page, "empty": empty}
+
+
+def _append(name, tokens, heads, dim, page, x, fused, skipped=0):
+    """fused: K and V are columns of one projection's output [tokens, 3 * heads * dim]; skipped: rows without a slot."""
+    return {"name": name, "kind": "append", "tokens": tokens, "heads": heads, "dim": dim, "page": page, "x": x, "fused": fused,
+            "skipped": skipped}
+
+
+def _attend(name, requests, past, new, heads, kv_heads, dim, page, x, lse=False, empty=0):
+    return {"name": name, "kind": "attend", "requests": requests, "past_lo": past[0], "past_hi": past[1], "new_lo": new[0],
+            "new_hi": new[1], "heads": heads, "kv_heads": kv_heads, "dim": dim, "page": page, "x": x, "lse": lse, "empty": empty}
+
+
+def listed():
+    return [
+        # every step of a decode loop over a small batch
+        _tables("tables_decode32", 32, (17, 2000), (1, 1), 16),
+        # a step of a busy server: prompts of all lengths beside single tokens, some slots of the batch idle
+        _tables("tables_mixed300", 300, (1, 8000), (1, 600), 32, empty=11),
+        # a small fp32 model, the new tokens of a small decode batch
+        _append("append_decode8", 8, 12, 64, 16, "f32", False),
+        # a ragged step, K and V still in the fused projection's rows, shared heads, a few rows of padding
+        _append("append_ragged333", 333, 8, 96, 32, "bf16", True, skipped=13),
+        # prefill of several prompts, one layer
+        _append("append_prefill8192", 8192, 32, 128, 64, "bf16", False),
+        # one sequence of a small fp32 model: launches and latency
+        _attend("token_small_f32", 1, (210, 210), (1, 1), 12, 12, 64, 16, "f32"),
+        # a ragged decode batch of 32 heads, one head of keys each, fp32 activations as the gated maps give them
+        _attend("decode64_ragged_f32", 64, (100, 4000), (1, 1), 32, 32, 128, 16, "f32", empty=3),
+        # two long contexts, shared heads; log sums beside the output, for a merge with other parts of a context
+        _attend("decode2_long_shared", 2, (60000, 131000), (1, 1), 32, 8, 128, 64, "bf16", lse=True),
+        # a few tokens a request (a draft that is checked), wide heads
+        _attend("few_tokens_wide_heads", 16, (500, 6000), (3, 5), 16, 16, 256, 32, "bf16"),
+        # a prompt from its first token
+        _attend("prefill2048", 1, (0, 0), (2048, 2048), 32, 32, 128, 64, "bf16"),
+        # ragged prompts behind cached prefixes, fp32 activations, shared heads of an odd width, one idle request
+        _attend("prefill_ragged_f32", 6, (50, 2000), (90, 700), 24, 8, 96, 16, "f32", empty=1),
+        # prompts taken in chunks, the last chunks of long ones
+        _attend("chunk512_long_shared", 4, (6000, 15000), (512, 512), 32, 8, 128, 128, "bf16"),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    kind = rng.choice(["tables", "append", "token", "batch", "batch", "long", "few", "prefill", "prefill", "chunk"])
+    page = rng.choice([16, 32, 64, 128])
+    x = rng.choice(["f32", "bf16"])
+    if kind == "tables":
+        requests = _log(rng, 1, 1500)
+        c = _tables("", requests, (rng.choice([0, 1, 30]), _log(rng, 40, 9000)), (1, _log(rng, 1, 2 + 40000 // requests)), page,
+                    empty=rng.choice([0, 0, requests // 9]))
+    elif kind == "append":
+        heads, dim = rng.choice([1, 4, 8, 12, 20, 32]), rng.choice([32, 64, 96, 128, 256])
+        tokens = _log(rng, 1, min(8192, (1 << 25) // (heads * dim)))
+        c = _append("", tokens, heads, dim, page, x, rng.random() < 0.5, skipped=rng.choice([0, 0, tokens // 7]))
+    else:
+        dim = rng.choice([64, 64, 96, 128, 128, 128, 160, 256])
+        kv_heads = rng.choice([1, 2, 4, 8, 8, 12, 16])
+        heads = kv_heads * rng.choice([1, 1, 2, 3, 4, 8] if kv_heads < 12 else [1, 2])
+        lse = rng.random() < 0.3
+        if kind == "token":
+            past, new, requests = (_log(rng, 1, 3000),) * 2, (1, 1), 1
+        elif kind == "batch":
+            requests = _log(rng, 2, 64)
+            hi = _log(rng, 50, min(6000, (1 << 28) // (requests * kv_heads * dim)))
+            past, new = (max(1, hi // rng.choice([1, 4, 30])), hi), (1, 1)
+        elif kind == "long":
+            requests = rng.choice([1, 1, 2, 3])
+            hi = _log(rng, 8000, min(131000, (1 << 28) // (requests * kv_heads * dim)))
+            past, new = (hi // rng.choice([1, 3]), hi), (1, 1)
+        elif kind == "few":
+            requests = _log(rng, 1, 24)
+            hi = _log(rng, 100, min(6000, (1 << 28) // (requests * kv_heads * dim)))
+            past, new = (hi // rng.choice([1, 5]), hi), (rng.choice([1, 2]), rng.choice([3, 4, 6, 8]))
+        elif kind == "prefill":
+            requests = _log(rng, 1, 8)
+            hi = _log(rng, 40, 2048 if requests == 1 else 1000)
+            past, new = rng.choice([(0, 0), (0, 0), (20, 1500)]), (max(1, hi // rng.choice([1, 1, 5])), hi)
+        else:
+            requests = _log(rng, 1, 4)
+            hi = _log(rng, 1000, 15000)
+            past, new = (hi // rng.choice([1, 2]), hi), (_log(rng, 60, 512),) * 2
+        c = _attend("", requests, past, new, heads, kv_heads, dim, page, x, lse, empty=1 if requests > 3 and rng.random() < 0.3 else 0)
+        while new[1] > 8 and work(c)["flops"] > 3e11:
+            kv_heads = max(1, kv_heads // 2)
+            c = dict(c, kv_heads=kv_heads, heads=kv_heads * max(1, min(8, c["heads"] // c["kv_heads"])))
+            if kv_heads == 1:
+                c["heads"] = min(c["heads"], 4)
+                break
+    del c["name"]
+    return c
+
+
+def _spread(n, lo, hi):
+    if n < 2 or lo == hi:
+        return [hi] * n
+    lo1 = max(lo, 1)
+    v = [int(round(lo1 * (hi / lo1) ** (i / (n - 1)))) for i in range(n)]
+    v[0] = lo
+    return v
+
+
+def _lengths(case):
+    """[(tokens in the cache before the step, new tokens)] of the requests, in a fixed order that mixes long with short."""
+    n = case["requests"] - case["empty"]
+    past, new = _spread(n, case["past_lo"], case["past_hi"]), _spread(n, case["new_lo"], case["new_hi"])
+    random.Random(7).shuffle(new)
+    return list(zip(past, new)) + [(0, 0)] * case["empty"]
+
+
+def work(case):
+    """What a pass cannot do without: every input that it needs read once, every output written once."""
+    if case["kind"] == "append":
+        n = (case["tokens"] - case["skipped"]) * case["heads"] * case["dim"] * 2      # elements of K and V
+        rows = case["tokens"] * case["heads"] * case["dim"] * 2
+        held = n * (BLOCK / 2 + 1) / BLOCK
+        return {"bytes": n * SIZE[case["x"]] + held + rows * SIZE[case["x"]] + 4 * case["tokens"], "flops": n}
+    ln = _lengths(case)
+    if case["kind"] == "tables":
+        p = case["page"]
+        pages = sum(-(-(a + b) // p) - (-(-a // p)) for a, b in ln)
+        return {"bytes": 8 * len(ln) + 8 * pages + 8 * len(ln) + 8 * sum(b for _, b in ln), "flops": 0}
+    keys = sum(a + b for a, b in ln if b)
+    pairs = sum(b * a + b * (b + 1) // 2 for a, b in ln)
+    rows = sum(b for _, b in ln) * case["heads"]
+    return {"bytes": keys * case["kv_heads"] * case["dim"] * 2 * (BLOCK / 2 + 1) / BLOCK + rows * (2 * case["dim"] * SIZE[case["x"]] + 4 * case["lse"]),
+            "flops": 4 * pairs * case["heads"] * case["dim"]}
+
+
+# ---- the 4-bit rows, in elementary operations ----------------------------------------------------------------
+def _quantise(x):
+    """x[..., dim] -> codes [..., dim / 2] and scales [..., dim / 32], both uint8."""
+    b = x.float().unflatten(-1, (-1, BLOCK))
+    most = b.abs().amax(-1)
+    # the smallest power of two with most / 2^e <= 6 = 1.5 * 4
+    scale = (((most.view(torch.int32) + 0x3FFFFF) >> 23) - 2).clamp(2, 254)
+    fine = torch.isfinite(b).all(-1)
+    a = torch.where(fine[..., None], b, 0.0) * torch.ldexp(torch.ones_like(most), 127 - scale)[..., None]
+    m = a.abs()
+    code = ((m > 0.25).int() + (m >= 0.75) + (m > 1.25) + (m >= 1.75) + (m > 2.5) + (m >= 3.5) + (m > 5.0)) | (torch.signbit(a).int() << 3)
+    code = code.flatten(-2).unflatten(-1, (-1, 2))
+    return (code[..., 0] | (code[..., 1] << 4)).to(torch.uint8), torch.where(fine, scale, 255).to(torch.uint8)
+
+
+def _values(codes, scales):
+    """codes [..., dim / 2], scales [..., dim / 32] -> fp32 [..., dim]"""
+    lut = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], device=codes.device)
+    lut = torch.cat([lut, -lut])
+    v = torch.stack([lut[(codes & 15).int()], lut[(codes >> 4).int()]], -1).flatten(-2)
+    s = scales.int()
+    s = torch.where(s < 255, torch.ldexp(torch.ones_like(s, dtype=torch.float32), s - 127), math.nan)
+    return (v.unflatten(-1, (-1, BLOCK)) * s[..., None]).flatten(-2)
+
+
+# ---- inputs -----------------------------------------------------------------------------------------------
+def _rows(g, n, heads, dim):
+    """Keys or values: normal, a few channels of a head several times as strong."""
+    strength = torch.exp(0.5 * torch.randn(heads, dim, generator=g, device=DEV))
+    return torch.randn(n, heads, dim, generator=g, device=DEV) * strength
+
+
+def _cache(g, pages, heads, page, dim):
+    """Pages full of rows: codes [pages, heads, page, dim / 2] and scales [pages, heads, dim / 32, page]."""
+    strength = torch.exp(0.5 * torch.randn(heads, 1, dim, generator=g, device=DEV))
+    codes = torch.empty(pages, heads, page, dim // 2, dtype=torch.uint8, device=DEV)
+    scales = torch.empty(pages, heads, dim // BLOCK, page, dtype=torch.uint8, device=DEV)
+    step = max(1, (1 << 26) // (heads * page * dim))
+    for i in range(0, pages, step):
+        c, s = _quantise(torch.randn(min(step, pages - i), heads, page, dim, generator=g, device=DEV) * strength)
+        codes[i:i + step], scales[i:i + step] = c, s.transpose(-1, -2)
+    return codes, scales
+
+
+def prepare(case, seed):
+    g = torch.Generator(device=DEV).manual_seed(int(seed))
+    i32 = dict(dtype=torch.int32, device=DEV)
+    page = case["page"]
+    if case["kind"] == "append":
+        n, heads, dim = case["tokens"], case["heads"], case["dim"]
+        K, V = _rows(g, n, heads, dim).to(TORCH[case["x"]]), _rows(g, n, heads, dim).to(TORCH[case["x"]])
+        if case["fused"]:
+            qkv = torch.zeros(n, 3, heads, dim, dtype=K.dtype, device=DEV)
+            qkv[:, 1], qkv[:, 2] = K, V
+            K, V = qkv[:, 1], qkv[:, 2]
+        pages = -(-n // page) + 3
+        cache = _cache(g, pages, heads, page, dim) + _cache(g, pages, heads, page, dim)
+        order = torch.randperm(pages, generator=g, device=DEV)[:-(-n // page)]
+        slots = (order[:, None] * page + torch.arange(page, device=DEV)).flatten()[:n].to(torch.int32)
+        if case["skipped"]:
+            slots[torch.randperm(n, generator=g, device=DEV)[:case["skipped"]]] = -1
+        return {"kind": "append", "cache": cache, "K": K, "V": V, "slots": slots}
+
+    ln = _lengths(case)
+    random.Random(int(seed)).shuffle(ln)
+    past, new = torch.tensor([a for a, _ in ln], **i32), torch.tensor([b for _, b in ln], **i32)
+    width = max(1, -(-max(a + b for a, b in ln) // page) + 1)
+    have = [-(-a // page) for a, _ in ln]
+    need = [-(-(a + b) // page) for a, b in ln]
+    tokens = sum(b for _, b in ln)
+    if case["kind"] == "tables":
+        total = sum(need) + 5
+        order = torch.randperm(total, generator=g, device=DEV).to(torch.int32)
+        owned = torch.arange(width, device=DEV)[None] < torch.tensor(have, device=DEV)[:, None]
+        table = torch.full((len(ln), width), -1, **i32)
+        table[owned] = order[:sum(have)]
+        free = order[sum(have):].contiguous()
+        # the slots' buffer has the length of the step's token budget
+        return {"kind": "tables", "past": past, "new": new, "free": free, "n_free": torch.tensor([free.numel()], **i32), "table": table,
+                "tokens": -(-max(tokens, 1) // 8) * 8, "page": page}
+    heads, kv_heads, dim = case["heads"], case["kv_heads"], case["dim"]
+    total = sum(need) + 2
+    cache = _cache(g, total, kv_heads, page, dim) + _cache(g, total, kv_heads, page, dim)
+    owned = torch.arange(width, device=DEV)[None] < torch.tensor(need, device=DEV)[:, None]
+    table = torch.full((len(ln), width), -1, **i32)
+    table[owned] = torch.randperm(total, generator=g, device=DEV)[:sum(need)].to(torch.int32)
+    start = torch.zeros(len(ln) + 1, **i32)
+    start[1:] = torch.cumsum(new, 0)
+    Q = (1.3 * torch.randn(tokens, heads, dim, generator=g, device=DEV)).to(TORCH[case["x"]])
+    return {"kind": "attend", "cache": cache, "Q": Q, "start": start, "len": past + new, "table": table, "lse": case["lse"],
+            "max_q": max(b for _, b in ln), "max_len": max(a + b for a, b in ln)}
+
+
+# ---- a pass ------------------------------------------------------------------------------------------------
+def run(s):
+    if own:
+        from paper_2605_03109_amd import gsi
+
+        if s["kind"] == "tables":
+            return (s["table"],) + tuple(gsi.kv_tables(s["past"], s["new"], s["free"], s["n_free"], s["table"], s["tokens"], s["page"]))
+        cache = gsi.KvCache(*s["cache"])
+        if s["kind"] == "append":
+            gsi.kv_append(cache, s["K"], s["V"], s["slots"])
+            return gsi.kv_expand(cache, s["slots"], s["K"].dtype)
+        return gsi.kv_attention(cache, s["Q"], s["start"], s["len"], s["table"], max_q=s["max_q"], max_len=s["max_len"], lse=s["lse"])
+    return {"tables": _plain_tables, "append": _plain_append, "attend": _plain_attend}[s["kind"]](s)
+
+
+def _plain_tables(s):
+    past, new, table, page, T = s["past"], s["new"], s["table"], s["page"], s["tokens"]
+    after = past + new
+    have, need = (past + page - 1) // page, (after + page - 1) // page
+    start = torch.zeros(past.numel() + 1, dtype=torch.int32, device=past.device)
+    start[1:] = torch.cumsum(new, 0)
+    first = torch.cumsum(need - have, 0) - (need - have)                       # of the free pages
+    j = torch.arange(table.shape[1], device=past.device)[None]
+    at = first[:, None] + j - have[:, None]
+    fresh = (j >= have[:, None]) & (j < need[:, None])
+    got = torch.where(at < s["n_free"], s["free"][at.clamp(0, s["free"].numel() - 1)], -1)
+    table.copy_(torch.where(fresh, got, table))
+    t = torch.arange(T, dtype=torch.int32, device=past.device)
+    r = torch.searchsorted(start[1:], t, right=True).clamp(max=past.numel() - 1)
+    pos = past[r] + t - start[r]
+    entry = table[r, (pos // page).clamp(max=table.shape[1] - 1)]
+    real = t < start[-1]
+    slots = torch.where(real & (entry >= 0), entry * page + pos % page, -1)
+    wanted = (need - have).sum(dtype=torch.int32)[None]
+    status = torch.cat([torch.minimum(wanted, s["n_free"]), (wanted - s["n_free"]).clamp(min=0)])
+    return table, after, start, slots, torch.where(real, pos, -1), status
+
+
+def _plain_append(s):
+    Kc, Ks, Vc, Vs = s["cache"]
+    page = Kc.shape[2]
+    real = s["slots"] >= 0
+    at = s["slots"][real].long()
+    p, o = at // page, at % page
+    out = []
+    for x, codes, scales in ((s["K"], Kc, Ks), (s["V"], Vc, Vs)):
+        c, e = _quantise(x)
+        codes[p, :, o] = c[real]
+        scales[p, :, :, o] = e[real]
+        out.append(torch.where(real[:, None, None], _values(c, e), 0.0).to(x.dtype))
+    return out
+
+
+def _plain_attend(s):
+    Kc, Ks, Vc, Vs = s["cache"]
+    Q, start, ln, table = s["Q"], s["start"].long(), s["len"], s["table"]
+    T, heads, dim = Q.shape
+    kv_heads, page = Kc.shape[1:3]
+    B, most = ln.numel(), s["max_q"]
+    table = table[:, :-(-s["max_len"] // page)].clamp(min=0).long()
+    L = table.shape[1] * page
+
+    def rows(codes, scales):                                                    # [B, kv_heads, L, dim]
+        v = _values(codes[table], scales[table].transpose(-1, -2))
+        return v.transpose(1, 2).reshape(B, kv_heads, L, dim)
+
+    n = start[1:] - start[:-1]
+    i = torch.arange(most, device=Q.device)
+    q = Q[(start[:-1, None] + i).clamp(max=T - 1)].float()                     # [B, most, heads, dim]
+    q = q.view(B, most, kv_heads, -1, dim).permute(0, 2, 3, 1, 4).reshape(B, kv_heads, -1, dim)
+    score = (q @ rows(Kc, Ks).transpose(-1, -2)).view(B, kv_heads, -1, most, L) * dim ** -0.5
+    seen = (ln - n)[:, None] + i[None]                                          # the last key that a token sees
+    keys = torch.arange(L, device=Q.device)
+    seen = (keys <= seen[..., None]) & (keys < ln[:, None, None])               # [B, most, L]
+    score = score.masked_fill(~seen[:, None, None], -math.inf)
+    top = score.amax(-1, keepdim=True)
+    top = torch.where(top == -math.inf, 0.0, top)
+    p = torch.exp(score - top)
+    total = p.sum(-1, keepdim=True)
+    v = rows(Vc, Vs)
+    out = (p.view(B, kv_heads, -1, L) @ v).view(B, kv_heads, -1, most, dim) / torch.where(total > 0, total, 1.0)
+    t = torch.arange(T, device=Q.device)
+    r = torch.searchsorted(start[1:], t, right=True)
+    out = out.permute(0, 3, 1, 2, 4).reshape(B, most, heads, dim)[r, t - start[r]].to(Q.dtype)
+    if not s["lse"]:
+        return out
+    lse = (top + torch.log(total))[..., 0].permute(0, 3, 1, 2).reshape(B, most, heads)
+    return out, lse[r, t - start[r]]
+
+
+# ---- what a pass returns, from the definitions in 64 bits -------------------------------------------------------
+def _exact_block(row):
+    """The 32 values that a block's row [n, 32] (float64) stands for once it is held."""
+    grid = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], dtype=torch.float64, device=row.device)
+    most = row.abs().amax(-1)
+    e = torch.ceil(torch.log2(most / 6.0))
+    e = torch.where(most > 6.0 * 2.0 ** e, e + 1, torch.where(most <= 6.0 * 2.0 ** (e - 1), e - 1, e)).clamp(min=-125)
+    unit = 2.0 ** e
+    a = row.abs() / unit[..., None]
+    hi = torch.bucketize(a, grid).clamp(max=7)                                  # the first grid value at or above
+    lo = (hi - 1).clamp(min=0)
+    down, up = a - grid[lo], grid[hi] - a
+    take = torch.where((up < down) | ((up == down) & (hi % 2 == 0)), hi, lo)    # nearest, ties to the even code
+    return torch.copysign(grid[take], row) * unit[..., None]
+
+
+def _exact_rows(codes, scales):
+    """Every value by sign, exponent and mantissa."""
+    c = torch.stack([codes % 16, codes // 16], -1).flatten(-2).to(torch.float64)
+    sign = 1 - 2 * (c >= 8).double()
+    c = c % 8
+    e, m = torch.div(c, 2, rounding_mode="floor"), c % 2
+    v = sign * torch.where(e > 0, (1 + m / 2) * 2.0 ** (e - 1), m / 2)
+    return v * torch.repeat_interleave(2.0 ** (scales.double() - 127), BLOCK, -1)
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    if case["kind"] == "append":
+        def held(x):
+            v = torch.cat([_exact_block(part.double().unflatten(-1, (-1, BLOCK))).flatten(-2) for part in x.split(512)])
+            return torch.where((s["slots"] >= 0)[:, None, None], v, torch.zeros((), dtype=torch.float64, device=v.device))
+        return [held(s["K"]), held(s["V"])]
+    if case["kind"] == "tables":
+        past, new, free, table = s["past"].tolist(), s["new"].tolist(), s["free"].tolist(), s["table"].tolist()
+        page, start, slots, positions, taken = s["page"], [0], [], [], 0
+        for a, b, row in zip(past, new, table):
+            for pos in range(a, a + b):
+                if row[pos // page] < 0:
+                    row[pos // page] = free[taken]
+                    taken += 1
+                slots.append(row[pos // page] * page + pos % page)
+                positions.append(pos)
+            start.append(len(slots))
+        pad = [-1] * (s["tokens"] - len(slots))
+        i32 = dict(dtype=torch.int32, device=DEV)
+        return tuple(torch.tensor(v, **i32) for v in (table, [a + b for a, b in zip(past, new)], start, slots + pad, positions + pad, [taken, 0]))
+    Kc, Ks, Vc, Vs = s["cache"]
+    heads, dim, page = case["heads"], case["dim"], case["page"]
+    group = heads // case["kv_heads"]
+    start, lens = s["start"].tolist(), s["len"].tolist()
+    out = torch.zeros(s["Q"].shape, dtype=torch.float64, device=DEV)
+    lse = torch.full(s["Q"].shape[:2], -math.inf, dtype=torch.float64, device=DEV)
+    for b, n in enumerate(lens):
+        t0, t1 = start[b], start[b + 1]
+        if t0 == t1:
+            continue
+        pages = s["table"][b, :-(-n // page)].long()
+        for h in range(case["kv_heads"]):
+            k = _exact_rows(Kc[pages, h], Ks[pages, h].transpose(-1, -2)).reshape(-1, dim)[:n]
+            v = _exact_rows(Vc[pages, h], Vs[pages, h].transpose(-1, -2)).reshape(-1, dim)[:n]
+            q = s["Q"][t0:t1, h * group:(h + 1) * group].double().transpose(0, 1)
+            z = (q @ k.t()) / math.sqrt(dim)
+            later = torch.triu(torch.ones(t1 - t0, n, dtype=torch.bool, device=DEV), n - (t1 - t0) + 1)
+            z.masked_fill_(later, -math.inf)
+            top = torch.logsumexp(z, -1)
+            out[t0:t1, h * group:(h + 1) * group] = (torch.exp(z - top[..., None]) @ v).transpose(0, 1)
+            lse[t0:t1, h * group:(h + 1) * group] = top.transpose(0, 1)
+    return (out, lse) if case["lse"] else out
