@@ -165,7 +165,7 @@ def _quantise(x):
     # the smallest power of two with most / 2^e <= 6 = 1.5 * 4
     scale = (((most.view(torch.int32) + 0x3FFFFF) >> 23) - 2).clamp(2, 254)
     fine = torch.isfinite(b).all(-1)
-    a = torch.where(fine[..., None], b, 0.0) * torch.ldexp(torch.ones_like(most), 127 - scale)[..., None]
+    a = torch.where(fine[..., None], b, 0.0) * ((254 - scale) << 23).view(torch.float32)[..., None]
     m = a.abs()
     code = ((m > 0.25).int() + (m >= 0.75) + (m > 1.25) + (m >= 1.75) + (m > 2.5) + (m >= 3.5) + (m > 5.0)) | (torch.signbit(a).int() << 3)
     code = code.flatten(-2).unflatten(-1, (-1, 2))
@@ -178,7 +178,7 @@ def _values(codes, scales):
     lut = torch.cat([lut, -lut])
     v = torch.stack([lut[(codes & 15).int()], lut[(codes >> 4).int()]], -1).flatten(-2)
     s = scales.int()
-    s = torch.where(s < 255, torch.ldexp(torch.ones_like(s, dtype=torch.float32), s - 127), math.nan)
+    s = torch.where(s < 255, (s << 23).view(torch.float32), math.nan)           # 2^(s - 127): the exponent field itself
     return (v.unflatten(-1, (-1, BLOCK)) * s[..., None]).flatten(-2)
 
 
