@@ -320,6 +320,66 @@ size_t gsi_layer_stack_workspace_bytes(const gsi_map_desc* maps, int32_t n_maps,
 size_t gsi_dense_stack_workspace_bytes(const gsi_map_desc* maps, int32_t n_maps, const gsi_input_desc* inputs,
                                        int32_t n_inputs, int64_t B);
 
+/* ---- The paged cache of keys and values in 4 bits, and attention over it -------------------------------------------
+ * What lies between the maps q, k, v of a block and its map o when tokens are served.  A request's tokens lie in pages of
+ * `page` tokens; table[r, j] names the page of its tokens j * page .. j * page + page - 1, and the slot of a token is
+ * page_id * page + offset.  A row (a token's 32 consecutive elements along a head) is held as E2M1 codes (1 sign, 2 exponent
+ * bits, 1 mantissa bit: 0 .5 1 1.5 2 3 4 6) with one scale 2^(byte - 127): the smallest power of two with
+ * max|x| / 2^e <= 6, byte 2 .. 254; codes are the nearest to x / 2^e, ties to the even code.  Byte 255 marks a block that
+ * had an element that is not finite: all its values are NaN.  Codes lie two to a byte, the even element in the low half.
+ * Limits: dim a multiple of 32 up to 256, page a power of two in 16 .. 4096, n_pages * page < 2^31. */
+typedef struct gsi_kv_cache {
+  uint8_t* K;         /* device, [n_pages, heads, page, dim / 2] codes of the keys, 16-byte aligned like the rest   */
+  uint8_t* K_scale;   /* device, [n_pages, heads, dim / 32, page]                                                   */
+  uint8_t* V;
+  uint8_t* V_scale;
+  int64_t n_pages;
+  int32_t heads;      /* of keys and values; queries may have a multiple of them                                    */
+  int32_t dim;        /* of a head                                                                                  */
+  int32_t page;
+  int32_t reserved;   /* 0                                                                                          */
+} gsi_kv_cache;
+
+/* Tables of one step, from the requests' lengths, on the device: B requests (at most 16384) with kv_len[b] tokens in the
+ * cache and n_new[b] tokens of this step.  Pages that a request lacks are taken from free_pages[0 .. n_free[0]) (at most
+ * free_cap entries are there), in the order of the requests, and entered in table[B, width]; entries that are there stay.
+ *   kv_len_out[b] = kv_len[b] + n_new[b];  q_start[0 .. B]: first token of each request among the step's tokens;
+ *   slots[t], positions[t] of the step's tokens t < q_start[B], -1 for the rest of T;
+ *   status[0] = pages taken, status[1] = pages that were wanted and not there (none free, or the table too narrow): their
+ *   entries and their tokens' slots are -1.
+ * Negative lengths count as 0; where the step has more than T tokens, the last are dropped from the requests' n_new.
+ * kv_len, n_new and free_pages are not changed: the caller's free list begins status[0] entries later.  No output may lie over an
+ * input.  The same call again gives the same results (the table's new entries are written again). */
+int gsi_kv_tables(const int32_t* kv_len, const int32_t* n_new, int64_t B, const int32_t* free_pages, const int32_t* n_free,
+                  int64_t free_cap, int32_t* table, int64_t width, int64_t page, int64_t T, int32_t* kv_len_out, int32_t* q_start,
+                  int32_t* slots, int32_t* positions, int32_t* status, void* stream);
+
+/* Rows of T tokens into the cache: K and V in `dtype`, token t at K + t * k_stride elements, its heads one after another
+ * [heads, dim]; slots[t] as above, a slot that is negative or past the cache's end is skipped.  No slot may come twice. */
+int gsi_kv_append(const gsi_kv_cache* cache, const void* K, const void* V, int64_t T, int64_t k_stride, int64_t v_stride, int dtype,
+                  const int32_t* slots, void* stream);
+
+/* The reverse: the values that the cache holds at slots[t], as K[T, heads, dim] and V in `dtype` (exact in both), 16-byte
+ * aligned.  Rows whose slot is negative or past the cache's end are zero. */
+int gsi_kv_expand(const gsi_kv_cache* cache, const int32_t* slots, int64_t T, void* K, void* V, int dtype, void* stream);
+
+/* Attention of the step's T tokens over their requests' keys, the step's own included: kv_len[b] keys in the pages of
+ * table[b, :], tokens q_start[b] .. q_start[b + 1] of which token i sees the keys j <= kv_len[b] - n + i (n tokens):
+ *   s_j = scale * q . k_j,   O[t, h] = sum_j softmax(s)_j v_j,   lse[t, h] = log sum_j exp(s_j)  (natural; NULL: not written).
+ * Q in `dtype`, token t at Q + t * q_stride elements, heads one after another; head h reads the keys of head
+ * h / (heads / cache->heads).  O[T, heads, dim] in `dtype`, 16-byte aligned.  A token that sees no key has O = 0, lse = -inf,
+ * and so have tokens from q_start[B] on.  Keys whose table entry names no page of the cache are not seen.  q_start NULL: every request has one token, B == T.
+ * max_q, max_len: the most new tokens and keys that a request is expected to have.  They choose kernels and their launches; other
+ * numbers cost time and never change what is computed.
+ * Arithmetic: keys are a matrix operand as they are held; queries are taken in 8-bit terms that sum to them (bf16 to 2^-22 of
+ * a block's largest element, fp32 to 2^-25); statistics and sums in fp32; the weights exp(s - max) enter the second product in bf16, once
+ * rounded (bf16 output) or in three terms (fp32 output).  ws: gsi_kv_attention_workspace_bytes(). */
+int gsi_kv_attention(const gsi_kv_cache* cache, const void* Q, int64_t T, int64_t heads, int64_t q_stride, int dtype,
+                     const int32_t* q_start, const int32_t* kv_len, int64_t B, const int32_t* table, int64_t width, int64_t max_q,
+                     int64_t max_len, float scale, void* O, float* lse, void* ws, size_t ws_bytes, void* stream);
+size_t gsi_kv_attention_workspace_bytes(const gsi_kv_cache* cache, int64_t T, int64_t heads, int dtype, int64_t B, int64_t max_q,
+                                        int64_t max_len);
+
 /* Number of bounded waits inside fused-kernel launches (GSI_INPUT_FUSED_KERNEL) on the current device that
  * expired since the library was loaded: 0 in normal operation; the outputs of a launch in which a wait expired
  * are not valid.  count: HOST pointer.  Synchronises the device. */

@@ -12,6 +12,7 @@
 #include "gsi_extend.h"
 #include "gsi_fused.h"
 #include "gsi_internal.h"
+#include "gsi_kv.h"
 #include "gsi_mfma.h"
 
 namespace {
@@ -1889,6 +1890,160 @@ int gsi_stack_plan_run(const gsi_stack_plan* plan, float eps, void* stream) {
   if (hipError_t e = gsi::stage_table_launch(rec.stage_table, rec.sg, eps, s); e != hipSuccess) return hip_fail(e, fn);
   if (hipError_t e = gsi::stream_fired_run(rec.fired_table, rec.fg, s); e != hipSuccess) return hip_fail(e, fn);
   return GSI_OK;
+}
+
+// ---- the paged cache in 4 bits -----------------------------------------------------------------------------
+static int check_cache(const char* fn, const gsi_kv_cache* c, gsi::KvView& v) {
+  if (c == nullptr) return fail(GSI_ERR_NULL, "%s: cache is NULL", fn);
+  if (!c->K || !c->K_scale || !c->V || !c->V_scale) return fail(GSI_ERR_NULL, "%s: the cache has a NULL buffer", fn);
+  if (c->heads < 1 || c->heads > 4096) return fail(GSI_ERR_SHAPE, "%s: need 1 <= heads <= 4096, got %d", fn, c->heads);
+  if (c->dim < 32 || c->dim > gsi::kKvMaxDim || c->dim % gsi::kKvBlock)
+    return fail(GSI_ERR_SHAPE, "%s: dim is a multiple of 32 up to %d, got %d", fn, gsi::kKvMaxDim, c->dim);
+  if (c->page < 16 || c->page > gsi::kKvMaxPage || (c->page & (c->page - 1)))
+    return fail(GSI_ERR_SHAPE, "%s: page is a power of two in 16 .. %d, got %d", fn, gsi::kKvMaxPage, c->page);
+  if (c->n_pages < 1 || c->n_pages > 0x7fffffff / c->page)
+    return fail(GSI_ERR_SHAPE, "%s: need 1 <= n_pages and n_pages * page < 2^31, got %lld pages", fn, (long long)c->n_pages);
+  if (c->reserved != 0) return fail(GSI_ERR_SHAPE, "%s: reserved is not 0", fn);
+  if (!aligned(c->K, 16) || !aligned(c->V, 16) || !aligned(c->K_scale, 16) || !aligned(c->V_scale, 16))
+    return fail(GSI_ERR_ALIGN, "%s: a buffer of the cache is not 16-byte aligned", fn);
+  v = gsi::KvView{c->K, c->K_scale, c->V, c->V_scale, c->n_pages, c->heads, c->dim, __builtin_ctz((unsigned)c->page)};
+  return GSI_OK;
+}
+static int check_tokens(const char* fn, int64_t T, int64_t row) {
+  if (T < 0 || T > (1ll << 30)) return fail(GSI_ERR_SHAPE, "%s: need 0 <= T <= 2^30, got %lld", fn, (long long)T);
+  if (gsi::ceil_div(T, 16) * gsi::ceil_div(row, 128) > 0x7fffffffll) return fail(GSI_ERR_SHAPE, "%s: too many tokens for one launch", fn);
+  return GSI_OK;
+}
+
+int gsi_kv_tables(const int32_t* kv_len, const int32_t* n_new, int64_t B, const int32_t* free_pages, const int32_t* n_free,
+                  int64_t free_cap, int32_t* table, int64_t width, int64_t page, int64_t T, int32_t* kv_len_out, int32_t* q_start,
+                  int32_t* slots, int32_t* positions, int32_t* status, void* stream) {
+  const char* fn = "gsi_kv_tables";
+  if (B < 0 || B > gsi::kKvMaxRequests)
+    return fail(GSI_ERR_SHAPE, "%s: need 0 <= B <= %lld, got %lld", fn, (long long)gsi::kKvMaxRequests, (long long)B);
+  if (T < 0 || T > (1ll << 30)) return fail(GSI_ERR_SHAPE, "%s: need 0 <= T <= 2^30, got %lld", fn, (long long)T);
+  if (page < 16 || page > gsi::kKvMaxPage || (page & (page - 1)))
+    return fail(GSI_ERR_SHAPE, "%s: page is a power of two in 16 .. %d, got %lld", fn, gsi::kKvMaxPage, (long long)page);
+  if (width < 1 || width > (1ll << 30)) return fail(GSI_ERR_SHAPE, "%s: need 1 <= width <= 2^30, got %lld", fn, (long long)width);
+  if (free_cap < 0 || free_cap > (1ll << 30)) return fail(GSI_ERR_SHAPE, "%s: need 0 <= free_cap <= 2^30, got %lld", fn, (long long)free_cap);
+  if (B == 0) return GSI_OK;
+  GSI_REQUIRE_PTR(kv_len);
+  GSI_REQUIRE_PTR(n_new);
+  GSI_REQUIRE_PTR(n_free);
+  if (free_cap > 0) GSI_REQUIRE_PTR(free_pages);
+  GSI_REQUIRE_PTR(table);
+  GSI_REQUIRE_PTR(kv_len_out);
+  GSI_REQUIRE_PTR(q_start);
+  if (T > 0) GSI_REQUIRE_PTR(slots);
+  if (T > 0) GSI_REQUIRE_PTR(positions);
+  GSI_REQUIRE_PTR(status);
+  for (const void* p : {(const void*)kv_len, (const void*)n_new, (const void*)free_pages, (const void*)n_free, (const void*)table,
+                        (const void*)kv_len_out, (const void*)q_start, (const void*)slots, (const void*)positions, (const void*)status})
+    if (!aligned(p, 4)) return fail(GSI_ERR_ALIGN, "%s: a pointer is not 4-byte aligned", fn);
+  if (kv_len_out == kv_len || kv_len_out == n_new)
+    return fail(GSI_ERR_SHAPE, "%s: kv_len_out lies over an input: workgroups read the lengths while others write", fn);
+  hipError_t e = gsi::kv_tables(kv_len, n_new, B, free_pages, n_free, free_cap, table, width, __builtin_ctzll((unsigned long long)page), T,
+                                kv_len_out, q_start, slots, positions, status, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? GSI_OK : hip_fail(e, fn);
+}
+
+int gsi_kv_append(const gsi_kv_cache* cache, const void* K, const void* V, int64_t T, int64_t k_stride, int64_t v_stride, int dtype,
+                  const int32_t* slots, void* stream) {
+  const char* fn = "gsi_kv_append";
+  gsi::KvView c;
+  if (int rc = check_cache(fn, cache, c)) return rc;
+  if (!dtype_ok(dtype)) return fail(GSI_ERR_DTYPE, "%s: unknown dtype %d", fn, dtype);
+  const int64_t row = (int64_t)c.heads * c.dim;
+  if (int rc = check_tokens(fn, T, row)) return rc;
+  if (T == 0) return GSI_OK;
+  GSI_REQUIRE_PTR(K);
+  GSI_REQUIRE_PTR(V);
+  GSI_REQUIRE_PTR(slots);
+  if (T > 1 && (k_stride < row || v_stride < row))
+    return fail(GSI_ERR_SHAPE, "%s: strides of %lld and %lld elements are less than a row of %lld", fn, (long long)k_stride, (long long)v_stride, (long long)row);
+  GSI_REQUIRE_ALIGNED(K, gsi::elem_size(dtype));
+  GSI_REQUIRE_ALIGNED(V, gsi::elem_size(dtype));
+  GSI_REQUIRE_ALIGNED(slots, 4);
+  hipError_t e = gsi::kv_append(c, K, V, T, k_stride, v_stride, dtype, slots, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? GSI_OK : hip_fail(e, fn);
+}
+
+int gsi_kv_expand(const gsi_kv_cache* cache, const int32_t* slots, int64_t T, void* K, void* V, int dtype, void* stream) {
+  const char* fn = "gsi_kv_expand";
+  gsi::KvView c;
+  if (int rc = check_cache(fn, cache, c)) return rc;
+  if (!dtype_ok(dtype)) return fail(GSI_ERR_DTYPE, "%s: unknown dtype %d", fn, dtype);
+  if (int rc = check_tokens(fn, T, (int64_t)c.heads * c.dim)) return rc;
+  if (T == 0) return GSI_OK;
+  GSI_REQUIRE_PTR(K);
+  GSI_REQUIRE_PTR(V);
+  GSI_REQUIRE_PTR(slots);
+  GSI_REQUIRE_ALIGNED(K, 16);
+  GSI_REQUIRE_ALIGNED(V, 16);
+  GSI_REQUIRE_ALIGNED(slots, 4);
+  hipError_t e = gsi::kv_expand(c, slots, T, K, V, dtype, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? GSI_OK : hip_fail(e, fn);
+}
+
+static int check_attend(const char* fn, const gsi_kv_cache* cache, int64_t T, int64_t heads, int dtype, int64_t B, int64_t max_q,
+                        int64_t max_len, gsi::KvAttend& a) {
+  if (int rc = check_cache(fn, cache, a.c)) return rc;
+  if (!dtype_ok(dtype)) return fail(GSI_ERR_DTYPE, "%s: unknown dtype %d", fn, dtype);
+  if (heads < 1 || heads > 65535 || heads % a.c.heads)
+    return fail(GSI_ERR_SHAPE, "%s: heads is a multiple of the cache's %d up to 65535, got %lld", fn, a.c.heads, (long long)heads);
+  if (T < 0 || T > (1ll << 30) || B < 0 || B > (1ll << 20))
+    return fail(GSI_ERR_SHAPE, "%s: need 0 <= T <= 2^30 and 0 <= B <= 2^20, got %lld and %lld", fn, (long long)T, (long long)B);
+  if (T * (heads / a.c.heads) > (1ll << 30)) return fail(GSI_ERR_SHAPE, "%s: more than 2^30 rows of a head of keys", fn);
+  if (max_q < 1 || max_len < 1) return fail(GSI_ERR_SHAPE, "%s: need max_q >= 1 and max_len >= 1", fn);
+  a.T = T;
+  a.heads = (int)heads;
+  a.dtype = dtype;
+  a.B = B;
+  a.max_q = std::min(max_q, std::max<int64_t>(T, 1));
+  a.max_len = std::min<int64_t>(max_len, 1ll << 30);
+  return GSI_OK;
+}
+
+int gsi_kv_attention(const gsi_kv_cache* cache, const void* Q, int64_t T, int64_t heads, int64_t q_stride, int dtype,
+                     const int32_t* q_start, const int32_t* kv_len, int64_t B, const int32_t* table, int64_t width, int64_t max_q,
+                     int64_t max_len, float scale, void* O, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  const char* fn = "gsi_kv_attention";
+  gsi::KvAttend a{};
+  if (int rc = check_attend(fn, cache, T, heads, dtype, B, max_q, max_len, a)) return rc;
+  if (T == 0) return GSI_OK;
+  GSI_REQUIRE_PTR(Q);
+  GSI_REQUIRE_PTR(O);
+  if (B > 0) GSI_REQUIRE_PTR(kv_len);
+  if (B > 0) GSI_REQUIRE_PTR(table);
+  if (width < 1 || width > (1ll << 30) / cache->page) return fail(GSI_ERR_SHAPE, "%s: need width >= 1 and width * page <= 2^30, got %lld", fn, (long long)width);
+  if (q_start == nullptr && B != T) return fail(GSI_ERR_SHAPE, "%s: without q_start every token is a request's only one: T = %lld, B = %lld", fn, (long long)T, (long long)B);
+  if (T > 1 && q_stride < heads * a.c.dim) return fail(GSI_ERR_SHAPE, "%s: q_stride of %lld elements is less than a row of %lld", fn, (long long)q_stride, (long long)(heads * a.c.dim));
+  if (!(scale > -3.0e38f && scale < 3.0e38f)) return fail(GSI_ERR_SHAPE, "%s: scale is not a finite number", fn);
+  GSI_REQUIRE_ALIGNED(Q, gsi::elem_size(dtype));
+  GSI_REQUIRE_ALIGNED(O, 16);
+  GSI_REQUIRE_ALIGNED(lse, 4);
+  GSI_REQUIRE_ALIGNED(q_start, 4);
+  GSI_REQUIRE_ALIGNED(kv_len, 4);
+  GSI_REQUIRE_ALIGNED(table, 4);
+  a.Q = Q;
+  a.q_stride = q_stride;
+  a.q_start = q_start;
+  a.kv_len = kv_len;
+  a.table = table;
+  a.width = width;
+  a.scale = scale;
+  a.O = O;
+  a.lse = lse;
+  if (int rc = check_ws(fn, ws, ws_bytes, gsi::kv_attention_workspace(a))) return rc;
+  hipError_t e = gsi::kv_attention(a, ws, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? GSI_OK : hip_fail(e, fn);
+}
+
+size_t gsi_kv_attention_workspace_bytes(const gsi_kv_cache* cache, int64_t T, int64_t heads, int dtype, int64_t B, int64_t max_q,
+                                        int64_t max_len) {
+  gsi::KvAttend a{};
+  if (check_attend("gsi_kv_attention_workspace_bytes", cache, T, heads, dtype, B, max_q, max_len, a) || T == 0) return 0;
+  return gsi::kv_attention_workspace(a);
 }
 
 }  // extern "C"

@@ -35,6 +35,7 @@ EXPORTS = (
     "gsi_stack_plan_bytes", "gsi_stack_plan_build", "gsi_stack_plan_run",
     "gsi_workspace_bytes", "gsi_layer_stack_workspace_bytes", "gsi_dense_stack_workspace_bytes", "gsi_last_error",
     "gsi_fused_timeouts",
+    "gsi_kv_tables", "gsi_kv_append", "gsi_kv_expand", "gsi_kv_attention", "gsi_kv_attention_workspace_bytes",
     "gsi_version",
 )
 
@@ -68,6 +69,14 @@ class ExtendDesc(ctypes.Structure):
         ("n_maps", ctypes.c_int32), ("k_cur", ctypes.c_void_p), ("R", ctypes.c_void_p), ("rnorm", ctypes.c_void_p),
         ("xnorm", ctypes.c_void_p), ("maps", ctypes.POINTER(ExtendMap)), ("gram", ctypes.c_void_p),
         ("extended", ctypes.c_void_p),
+    ]
+
+
+class KvCacheDesc(ctypes.Structure):
+    _fields_ = [
+        ("K", ctypes.c_void_p), ("K_scale", ctypes.c_void_p), ("V", ctypes.c_void_p), ("V_scale", ctypes.c_void_p),
+        ("n_pages", ctypes.c_int64), ("heads", ctypes.c_int32), ("dim", ctypes.c_int32), ("page", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
     ]
 
 
@@ -132,6 +141,15 @@ def _load() -> ctypes.CDLL:
     lib.gsi_dense_stack_workspace_bytes.restype = sz
     lib.gsi_fused_timeouts.argtypes = [ctypes.POINTER(ctypes.c_uint32)]
     lib.gsi_fused_timeouts.restype = ctypes.c_int
+    kvp = ctypes.POINTER(KvCacheDesc)
+    lib.gsi_kv_tables.argtypes = [vp, vp, i64, vp, vp, i64, vp, i64, i64, i64, vp, vp, vp, vp, vp, vp]
+    lib.gsi_kv_append.argtypes = [kvp, vp, vp, i64, i64, i64, i32, vp, vp]
+    lib.gsi_kv_expand.argtypes = [kvp, vp, i64, vp, vp, i32, vp]
+    lib.gsi_kv_attention.argtypes = [kvp, vp, i64, i64, i64, i32, vp, vp, i64, vp, i64, i64, i64, f32, vp, vp, vp, sz, vp]
+    for name in ("gsi_kv_tables", "gsi_kv_append", "gsi_kv_expand", "gsi_kv_attention"):
+        getattr(lib, name).restype = ctypes.c_int
+    lib.gsi_kv_attention_workspace_bytes.argtypes = [kvp, i64, i64, i32, i64, i64, i64]
+    lib.gsi_kv_attention_workspace_bytes.restype = sz
     lib.gsi_last_error.restype = ctypes.c_char_p
     lib.gsi_version.restype = ctypes.c_int
     for name in ("gsi_build_image", "gsi_build_gram", "gsi_quantize_image_fp8", "gsi_project", "gsi_gate", "gsi_gated_linear", "gsi_dense_linear",
@@ -509,3 +527,120 @@ def layer_stack(inputs: Sequence[dict], maps: Sequence[dict], B: int, eps: float
     st = LayerStack(inputs, maps, B, eps)
     st.run(stream)
     return st
+
+
+# ----------------------------------------------------------------------------------------------
+# the paged cache of keys and values in 4 bits, and attention over it
+# ----------------------------------------------------------------------------------------------
+class KvCache:
+    """The buffers of a paged cache (uint8 device tensors): codes K, V [n_pages, heads, page, dim / 2] and scales
+    K_scale, V_scale [n_pages, heads, dim / 32, page]."""
+
+    __slots__ = ("K", "K_scale", "V", "V_scale", "heads", "dim", "page", "desc")
+
+    def __init__(self, K: torch.Tensor, K_scale: torch.Tensor, V: torch.Tensor, V_scale: torch.Tensor):
+        n, heads, page, half = K.shape
+        if V.shape != K.shape or K_scale.shape != (n, heads, half // 16, page) or V_scale.shape != K_scale.shape:
+            raise ValueError("K, V[n_pages, heads, page, dim/2] and K_scale, V_scale[n_pages, heads, dim/32, page] must agree")
+        if not K.dtype == V.dtype == K_scale.dtype == V_scale.dtype == torch.uint8:
+            raise ValueError("codes and scales are uint8")
+        self.K, self.K_scale, self.V, self.V_scale = K, K_scale, V, V_scale
+        self.heads, self.dim, self.page = heads, 2 * half, page
+        self.desc = KvCacheDesc(_ptr(K), _ptr(K_scale), _ptr(V), _ptr(V_scale), n, heads, 2 * half, page, 0)
+
+    @classmethod
+    def empty(cls, n_pages: int, heads: int, dim: int, page: int, device="cuda") -> "KvCache":
+        """A cache without rows (all bytes zero)."""
+        u8 = dict(dtype=torch.uint8, device=device)
+        codes, scales = (n_pages, heads, page, dim // 2), (n_pages, heads, dim // 32, page)
+        return cls(torch.zeros(codes, **u8), torch.zeros(scales, **u8), torch.zeros(codes, **u8), torch.zeros(scales, **u8))
+
+
+def _i32(name: str, t: torch.Tensor, n: Optional[int] = None) -> int:
+    """Pointer of an int32 device tensor (of n elements)."""
+    if t.dtype != torch.int32 or (n is not None and t.numel() != n):
+        raise ValueError(f"{name} must be int32" + ("" if n is None else f" with {n} elements") + f", got {t.dtype} {tuple(t.shape)}")
+    return _ptr(t)
+
+
+def _rows_of_heads(name: str, t: torch.Tensor, dim: int) -> Tuple[int, int]:
+    """(pointer, elements between tokens) of t[T, heads, dim] whose tokens may lie further apart than a row."""
+    if not t.is_cuda:
+        raise ValueError("libgsi takes device tensors only")
+    if t.dim() != 3 or t.shape[2] != dim or (t.stride(2) != 1 and dim != 1) or (t.stride(1) != dim and t.shape[1] != 1):
+        raise ValueError(f"{name}[T, heads, {dim}] must hold the heads of a token one after another, got {tuple(t.shape)} with strides {t.stride()}")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1] * dim
+
+
+def kv_tables(kv_len: torch.Tensor, n_new: torch.Tensor, free_pages: torch.Tensor, n_free: torch.Tensor, table: torch.Tensor,
+              T: int, page: int, stream=None):
+    """Tables of one step: fills the missing entries of table[B, width] in place from the free list and returns
+    (kv_len_out[B], q_start[B + 1], slots[T], positions[T], status[2]); all tensors int32."""
+    B = kv_len.numel()
+    if table.dim() != 2 or table.shape[0] != B:
+        raise ValueError(f"table must be [{B}, width], got {tuple(table.shape)}")
+    out = torch.empty((2 * B + 1 + 2 * T + 2,), dtype=torch.int32, device=table.device)
+    new_len, start, slots, positions, status = out.split((B, B + 1, T, T, 2))
+    if B == 0:
+        start.zero_(), slots.fill_(-1), positions.fill_(-1), status.zero_()
+    base = out.data_ptr()
+    _check(lib.gsi_kv_tables(_i32("kv_len", kv_len), _i32("n_new", n_new, B), B, _i32("free_pages", free_pages), _i32("n_free", n_free, 1),
+                             free_pages.numel(), _i32("table", table), table.shape[1], page, T, base, base + 4 * B,
+                             base + 4 * (2 * B + 1), base + 4 * (2 * B + 1 + T), base + 4 * (2 * B + 1 + 2 * T), _stream(stream)))
+    return new_len, start, slots, positions, status
+
+
+def kv_append(cache: KvCache, K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor, stream=None) -> None:
+    """Rows K, V[T, heads, dim] (fp32 or bf16; tokens may lie further apart than a row) into the cache at slots[T]."""
+    T = K.shape[0]
+    if K.shape != V.shape or K.dtype != V.dtype or K.shape[1] != cache.heads:
+        raise ValueError(f"K and V[T, {cache.heads}, {cache.dim}] must agree in shape and dtype")
+    (kp, ks), (vp, vs) = _rows_of_heads("K", K, cache.dim), _rows_of_heads("V", V, cache.dim)
+    _check(lib.gsi_kv_append(ctypes.byref(cache.desc), kp, vp, T, ks, vs, dtype_code(K), _i32("slots", slots, T), _stream(stream)))
+
+
+def kv_expand(cache: KvCache, slots: torch.Tensor, dtype: torch.dtype = torch.float32, K=None, V=None, stream=None):
+    """The values that the cache holds at slots[T]: K, V[T, heads, dim] in `dtype`; zero rows for negative slots."""
+    shape = (slots.numel(), cache.heads, cache.dim)
+    K = torch.empty(shape, dtype=dtype, device=slots.device) if K is None else K
+    V = torch.empty(shape, dtype=dtype, device=slots.device) if V is None else V
+    if tuple(K.shape) != shape or tuple(V.shape) != shape or K.dtype != V.dtype:
+        raise ValueError(f"K and V must be {shape} of one dtype")
+    _check(lib.gsi_kv_expand(ctypes.byref(cache.desc), _i32("slots", slots), slots.numel(), _ptr(K), _ptr(V), dtype_code(K), _stream(stream)))
+    return K, V
+
+
+def kv_attention(cache: KvCache, Q: torch.Tensor, q_start: Optional[torch.Tensor], kv_len: torch.Tensor, table: torch.Tensor,
+                 max_q: Optional[int] = None, max_len: Optional[int] = None, scale: Optional[float] = None, O=None, lse=None,
+                 ws=None, stream=None):
+    """Attention of Q[T, heads, dim] (fp32 or bf16; tokens may lie further apart than a row) over the cache: O[T, heads, dim], or
+    (O, lse[T, heads]) where ``lse`` is True or a tensor.  q_start None: one token a request.  max_q, max_len: what the
+    requests are expected to have at most (default: what the shapes allow); scale: 1 / sqrt(dim) by default."""
+    T, heads, dim = Q.shape
+    B = kv_len.numel()
+    if dim != cache.dim:
+        raise ValueError(f"Q has heads of {dim} elements, the cache of {cache.dim}")
+    if table.dim() != 2 or table.shape[0] != B:
+        raise ValueError(f"table must be [{B}, width], got {tuple(table.shape)}")
+    qp, qs = _rows_of_heads("Q", Q, dim)
+    O = torch.empty((T, heads, dim), dtype=Q.dtype, device=Q.device) if O is None else O
+    if tuple(O.shape) != (T, heads, dim) or O.dtype != Q.dtype:
+        raise ValueError("O must have Q's shape and dtype")
+    if lse is True:
+        lse = torch.empty((T, heads), dtype=torch.float32, device=Q.device)
+    elif lse is False:
+        lse = None
+    if lse is not None and (tuple(lse.shape) != (T, heads) or lse.dtype != torch.float32):
+        raise ValueError("lse must be fp32 [T, heads]")
+    if max_q is None:
+        max_q = 1 if q_start is None else max(T, 1)
+    if max_len is None:
+        max_len = table.shape[1] * cache.page
+    dt, desc = dtype_code(Q), ctypes.byref(cache.desc)
+    max_q, max_len = max(int(max_q), 1), max(int(max_len), 1)
+    need = int(lib.gsi_kv_attention_workspace_bytes(desc, T, heads, dt, B, max_q, max_len))
+    wsp, wsn, held = _ws_args(ws, need, stream)
+    _check(lib.gsi_kv_attention(desc, qp, T, heads, qs, dt, None if q_start is None else _i32("q_start", q_start, B + 1),
+                                _i32("kv_len", kv_len), B, _i32("table", table), table.shape[1], max_q, max_len,
+                                dim ** -0.5 if scale is None else float(scale), _ptr(O), _ptr(lse), wsp, wsn, _stream(stream)))
+    return O if lse is None else (O, lse)
