@@ -371,9 +371,8 @@ int gsi_kv_expand(const gsi_kv_cache* cache, const int32_t* slots, int64_t T, vo
  * and so have tokens from q_start[B] on.  Keys whose table entry names no page of the cache are not seen.  q_start NULL: every request has one token, B == T.
  * max_q, max_len: the most new tokens and keys that a request is expected to have.  They choose kernels and their launches; other
  * numbers cost time and never change what is computed.
- * Arithmetic: keys are a matrix operand as they are held; queries are taken in 8-bit terms that sum to them (bf16 to 2^-22 of
- * a block's largest element, fp32 to 2^-25); statistics and sums in fp32; the weights exp(s - max) enter the second product in bf16, once
- * rounded (bf16 output) or in three terms (fp32 output).  ws: gsi_kv_attention_workspace_bytes(). */
+ * Arithmetic: fp32 sums and statistics of bf16 products; keys and values are exact in bf16, queries and weights exp(s - max) enter in
+ * one bf16 term (bf16: a query itself, a weight rounded once) or in three (fp32). ws: gsi_kv_attention_workspace_bytes(). */
 int gsi_kv_attention(const gsi_kv_cache* cache, const void* Q, int64_t T, int64_t heads, int64_t q_stride, int dtype,
                      const int32_t* q_start, const int32_t* kv_len, int64_t B, const int32_t* table, int64_t width, int64_t max_q,
                      int64_t max_len, float scale, void* O, float* lse, void* ws, size_t ws_bytes, void* stream);

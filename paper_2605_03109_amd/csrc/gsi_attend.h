@@ -1,0 +1,73 @@
+// Device code that the attention kernels over the 4-bit cache share (gsi_attend.hip, gsi_prompt.hip).
+#pragma once
+#include "gsi_device.h"
+#include "gsi_kv.h"
+
+namespace gsi {
+
+// Launches of the two kernels, each for its own requests: those of at most `few` rows of a head of keys (tokens times the heads
+// that share it) and those of more.
+hipError_t attend_few(const KvAttend& a, int64_t few, void* ws, hipStream_t s);
+size_t attend_few_workspace(const KvAttend& a, int64_t few);
+
+namespace {
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8;
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+// The running maximum of a row moves only when a score passes it by more than 2^kSlack in the exponential: weights stay below
+// 2^kSlack, which costs fp32 sums and bf16 weights nothing, and almost no step rescales what is summed so far.
+constexpr float kSlack = 8.f;
+
+struct Span {  // a request's tokens of the call and its keys
+  int t0, n, len;
+};
+__device__ __forceinline__ Span span_of(const KvAttend& a, int b) {
+  Span s;
+  const int T = (int)a.T;
+  s.t0 = a.q_start ? min(max(a.q_start[b], 0), T) : min(b, T);
+  const int t1 = a.q_start ? min(max(a.q_start[b + 1], s.t0), T) : min(b + 1, T);
+  s.n = t1 - s.t0;
+  s.len = (int)min((int64_t)max(a.kv_len[b], 0), a.width << a.c.page_shift);
+  return s;
+}
+
+__device__ __forceinline__ float scale_value(int byte) { return __uint_as_float((uint32_t)byte << 23); }
+// 16 elements of a query row from element d on; zero past the head's end or for no row
+template <class X>
+__device__ __forceinline__ void load_q16(const typename X::storage* row, int d, bool ok, bool wide, float (&x)[16]) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) x[i] = 0.f;
+  if (!ok) return;
+  if (wide) {
+#pragma unroll
+    for (int i = 0; i < 16; i += X::kVec) X::load_vec(row + d + i, reinterpret_cast<float(&)[X::kVec]>(x[i]));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = X::load(row, d + i);
+  }
+}
+
+__device__ __forceinline__ float row16_max(float v) {  // over aligned groups of 16 lanes
+  v = fmaxf(v, dpp_move<0xB1>(v));
+  v = fmaxf(v, dpp_move<0x4E>(v));
+  v = fmaxf(v, dpp_move<0x141>(v));
+  return fmaxf(v, dpp_move<0x140>(v));
+}
+__device__ __forceinline__ float row16_sum(float v) {
+  v += dpp_move<0xB1>(v);
+  v += dpp_move<0x4E>(v);
+  v += dpp_move<0x141>(v);
+  return v + dpp_move<0x140>(v);
+}
+
+__device__ __forceinline__ void order_lds() { asm volatile("" ::: "memory"); }  // a wave's LDS accesses run in program order
+
+}  // namespace
+}  // namespace gsi
