@@ -9,6 +9,8 @@ namespace gsi {
 // that share it) and those of more.
 hipError_t attend_few(const KvAttend& a, int64_t few, void* ws, hipStream_t s);
 size_t attend_few_workspace(const KvAttend& a, int64_t few);
+hipError_t attend_prompt(const KvAttend& a, int64_t few, bool zero, void* ws, hipStream_t s);  // zero: it writes the tokens of no request
+size_t attend_prompt_workspace(const KvAttend& a);
 
 namespace {
 

@@ -644,8 +644,33 @@ hipError_t attend_few(const KvAttend& a, int64_t few, void* ws, hipStream_t s) {
   return hipGetLastError();
 }
 
-size_t kv_attention_workspace(const KvAttend& a) { return attend_few_workspace(a, INT64_MAX); }
+// Which kernels a call takes.  Requests of at most kFewRows rows of a head of keys are cheaper where a workgroup has 16 rows; where no
+// request is expected to have more, those take all of them, and where the requests are about of one length, or few rows are
+// not expected at all, the others do.
+constexpr int64_t kFewRows = 32;
+enum Kernels { kFewOnly, kPromptOnly, kBoth };
+static Kernels kernels_of(const KvAttend& a) {
+  const int64_t most = std::min(a.max_q, a.T);
+  if (most * (a.heads / a.c.heads) <= kFewRows || a.B == 0) return kFewOnly;
+  return 2 * a.T >= a.B * most ? kPromptOnly : kBoth;
+}
 
-hipError_t kv_attention(const KvAttend& a, void* ws, hipStream_t s) { return attend_few(a, INT64_MAX, ws, s); }
+size_t kv_attention_workspace(const KvAttend& a) {
+  switch (kernels_of(a)) {
+    case kFewOnly: return attend_few_workspace(a, INT64_MAX);
+    case kPromptOnly: return attend_prompt_workspace(a);
+    default: return attend_few_workspace(a, kFewRows) + attend_prompt_workspace(a);
+  }
+}
+
+hipError_t kv_attention(const KvAttend& a, void* ws, hipStream_t s) {
+  switch (kernels_of(a)) {
+    case kFewOnly: return attend_few(a, INT64_MAX, ws, s);
+    case kPromptOnly: return attend_prompt(a, 0, true, ws, s);
+    default: break;
+  }
+  if (hipError_t e = attend_few(a, kFewRows, ws, s); e != hipSuccess) return e;
+  return attend_prompt(a, kFewRows, false, static_cast<char*>(ws) + attend_few_workspace(a, kFewRows), s);
+}
 
 }  // namespace gsi
