@@ -1,10 +1,11 @@
 // Attention over the paged cache in 4 bits, few rows: single tokens, and a few tokens of a request.
 //
 // For a row (a token and a head) with query q: s_j = scale q.k_j over the keys that it sees, o = sum_j 2^(s_j' - m) v_j / sum_j 2^(s_j' - m),
-// s' = s log2 e, m a running maximum.  A workgroup takes up to 16 rows that share a head of keys and 256 keys at a time, 64 a
-// wave.  Both products are bf16 matrix products of codes times scales (exact in bf16).  A lane loads 32 consecutive codes of a key, which
-// are its operands of four products over 8 elements each, and 4, 8 or 16 elements of eight consecutive values, which
-// are the rows of as many products over 32 tokens: neither keys nor values need a transposition through LDS.
+// s' = s log2 e, m a running maximum.  A wave takes up to 16 rows that share a head of keys and 64 keys a step.  Both products are
+// bf16 matrix products of codes times scales (exact in bf16), and neither operand is transposed: a lane loads 16, 32 or 64 consecutive
+// codes of a key, its operands of products over 8 elements each, and 4, 8 or 16 elements of 16 consecutive values.  A pair
+// of those as it is converted, two elements of one token, is a pair of the contraction: the weights of a row are given twice,
+// once with zeros against the odd elements and once with zeros against the even ones, as two rows of the product.
 #include <algorithm>
 
 #include "gsi_attend.h"
@@ -13,241 +14,230 @@ namespace gsi {
 namespace {
 
 constexpr int kWaves = 4, kThreads = kWaves * kWave;
-constexpr int kStep = 64;               // keys of a wave and step
-constexpr int kUnit = kWaves * kStep;   // keys of a workgroup and step: the unit in which the work is dealt out
-constexpr int kRows = 16;               // rows of the products
-constexpr int kPStride = kStep + 8;     // bf16 elements of a row of weights in LDS
+constexpr int kStep = 64;             // keys of a wave and step: the unit in which the work is dealt out
+constexpr int kPStride = kStep + 4;   // bf16 weights of a row in LDS
+constexpr int kManyParts = 12;        // parts of a tile that one wave joins by itself
 
 struct Few {
   KvAttend a;
   int64_t few;    // requests of more rows are another kernel's
   int group;      // heads that share a head of keys
-  int tile_rows;  // rows of a tile: 4, 8 or 16
+  int tile_rows;  // rows of a tile
   int q_wide;     // 16-byte loads of queries
-  float* parts;   // [2 * workgroups][tile_rows][dim + 2]: sums, maximum, sum of weights of a cut tile
-  int* heads;     // [workgroups][4]: the tile that a workgroup begins and does not end, and the workgroup that ends it
+  int whole;      // a workgroup takes whole tiles, its waves parts of their keys; else every wave an equal share of all steps
+  float* parts;   // [2 * waves][tile_rows][dim + 2]: sums, maximum, sum of weights of a cut tile
+  int* cuts;      // [waves][4]: the tile that a wave begins and does not end, and the wave that ends it
+  int* joined;    // [workgroups]: whether its waves' parts are in the first one's place
 };
 
-__device__ __forceinline__ int rows_of(const Few& f, const Span& s) {
+// Tiles of a request and the steps of each (one where there are rows but no keys).  A tile counts as kTileCost units and one for every step: its
+// queries, first loads and output cost a wave about as much as so many steps.
+constexpr int kTileCost = 2;
+struct Steps {
+  int tiles, per_tile;
+};
+__device__ __forceinline__ Steps steps_of(const Few& f, const Span& s) {
   const int64_t rows = (int64_t)s.n * f.group;
-  return rows <= f.few ? (int)rows : 0;
+  return Steps{rows <= f.few ? (int)((uint32_t)(rows + f.tile_rows - 1) / (uint32_t)f.tile_rows) : 0, max(1, (s.len + kStep - 1) / kStep)};
 }
-// Units of a request: tiles of rows, times heads of keys, times units of keys (one where there are rows but no keys)
-__device__ __forceinline__ int64_t units_of(const Few& f, const Span& s, int& per_tile, int& tiles) {
-  tiles = (rows_of(f, s) + f.tile_rows - 1) / f.tile_rows;
-  per_tile = max(1, (s.len + kUnit - 1) / kUnit);
-  return (int64_t)tiles * f.a.c.heads * per_tile;
+__device__ __forceinline__ int tile_units(const Few& f, const Steps& st) { return f.whole ? 1 : st.per_tile + kTileCost; }
+
+__device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {  // both at least 0; the quotient of 64 bits takes a hundred instructions
+  return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
 }
 
-// The units of all requests, and the request that unit `u` lies in with the units before it.  One round of loads up to 256 requests.
-struct Place {
-  int64_t total, before;
-  int b;
+// The spans of 256 requests at a time, and prefix sums of their units, in LDS.
+struct Prefix {
+  int64_t incl[kThreads];
+  int64_t sums[kWaves];
+  Span span[kThreads];
 };
-__device__ __forceinline__ int64_t wave_scan(int64_t v) {
-  const int lane = threadIdx.x % kWave;
+__device__ __forceinline__ int64_t scan_requests(const Few& f, int64_t b0, Prefix& x) {
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int64_t b = b0 + threadIdx.x;
+  int64_t v = 0;
+  Span sp{0, 0, 0};
+  if (b < f.a.B) {
+    sp = span_of(f.a, (int)b);
+    const Steps st = steps_of(f, sp);
+    v = (int64_t)st.tiles * f.a.c.heads * tile_units(f, st);
+  }
 #pragma unroll
   for (int o = 1; o < kWave; o <<= 1) {
     const int64_t up = __shfl_up(v, o, kWave);
     if (lane >= o) v += up;
   }
-  return v;
-}
-__device__ __forceinline__ int64_t total_units(const Few& f, int64_t* lds) {
-  int64_t sum = 0;
-  int per, tiles;
-  for (int64_t b = threadIdx.x; b < f.a.B; b += kThreads) sum += units_of(f, span_of(f.a, (int)b), per, tiles);
-  sum = wave_scan(sum);
   __syncthreads();
-  if (threadIdx.x % kWave == kWave - 1) lds[threadIdx.x / kWave] = sum;
+  if (lane == kWave - 1) x.sums[wave] = v;
   __syncthreads();
-  return lds[0] + lds[1] + lds[2] + lds[3];
-}
-__device__ __forceinline__ Place place_of_unit(const Few& f, int64_t u, int64_t* lds) {
-  // lds: [0..3] sums of the waves, [4] request, [5] units before it
-  Place p{0, 0, 0};
-  int64_t carry = 0;
-  for (int64_t b0 = 0; b0 < f.a.B; b0 += kThreads) {
-    const int64_t b = b0 + threadIdx.x;
-    int per, tiles;
-    const int64_t mine = b < f.a.B ? units_of(f, span_of(f.a, (int)b), per, tiles) : 0;
-    const int64_t incl = wave_scan(mine);
-    __syncthreads();
-    if (threadIdx.x % kWave == kWave - 1) lds[threadIdx.x / kWave] = incl;
-    __syncthreads();
-    int64_t at = carry;
-    for (int w = 0; w < (int)threadIdx.x / kWave; ++w) at += lds[w];
-    const int64_t before = at + incl - mine;
-    if (u >= before && u < before + mine) {
-      lds[4] = b;
-      lds[5] = before;
-    }
-    carry += lds[0] + lds[1] + lds[2] + lds[3];
-    if (u < carry) break;  // the same for every thread
+  int64_t total = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < wave) v += x.sums[w];
+    total += x.sums[w];
   }
+  x.incl[threadIdx.x] = v;
+  x.span[threadIdx.x] = sp;
   __syncthreads();
-  p.b = (int)lds[4];
-  p.before = lds[5];
-  __syncthreads();
-  return p;
+  return total;
+}
+// (the first 256 requests' spans stay in LDS unless there are more requests)
+__device__ __forceinline__ Span span_at(const Few& f, const Prefix& x, int b) { return f.a.B <= kThreads ? x.span[b] : span_of(f.a, b); }
+
+// Wave i of the launch takes the units [first_unit(i), first_unit(i + 1)): equal shares for the workgroups, four units at least, and
+// for their waves.  No wave before the last that has any is without one.
+struct Shares {
+  int64_t total, groups, each, more;  // each: units of a workgroup; the first `more` have one more
+  __device__ __forceinline__ int64_t of_group(int64_t g) const { return each * g + min(g, more); }
+  __device__ __forceinline__ int64_t first_unit(int64_t i) const {
+    const int64_t g = i / kWaves, k = i % kWaves;
+    if (total < kWaves) return min(i, total);
+    return of_group(g) + (each + (g < more ? 1 : 0)) * k / kWaves;
+  }
+  __device__ __forceinline__ int64_t owner(int64_t u) const {  // the wave that has unit u
+    const int64_t big = more * (each + 1);
+    const int64_t g = total < kWaves ? 0 : u < big ? divide(u, each + 1) : more + divide(u - big, each);
+    int64_t i = g * kWaves + kWaves - 1;
+    while (first_unit(i) > u) --i;
+    return i;
+  }
+};
+__device__ __forceinline__ Shares shares_of(int64_t total, int64_t groups) {
+  groups = max((int64_t)1, min(groups, total / kWaves));
+  const int64_t each = divide(total, groups);
+  return Shares{total, groups, each, total - each * groups};
 }
 
-// ---- a step's operands: 64 keys and values ------------------------------------------------------------------
+// ---- operands -------------------------------------------------------------------------------------------------
 template <int DPL>
-struct VWord;  // the codes of a lane's DPL elements of a token
+struct VWord;  // the codes of a lane's DPL elements of a value
 template <> struct VWord<4> { using type = uint16_t; };
 template <> struct VWord<8> { using type = uint32_t; };
 template <> struct VWord<16> { using type = u32x2; };
-
-template <int DPL>
-struct Step {
-  static constexpr int DC = DPL == 16 ? 2 : 1;  // products of 128 elements of a key
-  u32x4 k[DC][4];     // token 4 c + j of lane c's block
-  uint32_t ks[DC];    // its four scale bytes
-  typename VWord<DPL>::type v[2][8];
-  u32x2 vs[2];
-};
-
-struct Pages {  // page ids of a lane's keys and of its two groups of eight values; as the table has them
-  int k, v[2];
-};
-
-template <int DPL>
-struct Lane {  // where a lane's operands lie
-  int c, g;         // lane % 16, lane / 16
-  int kblk[2];      // blocks of 32 elements of a key (held in range)
-  bool kreal[2];
-  int vd;           // first element of its values (held in range)
-  __device__ __forceinline__ Lane(int dim) {
-    const int lane = threadIdx.x % kWave;
-    c = lane % 16;
-    g = lane / 16;
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      kreal[x] = (g + 4 * x) * kKvBlock < dim;
-      kblk[x] = kreal[x] ? g + 4 * x : 0;
-    }
-    vd = c * DPL < dim ? c * DPL : 0;
-  }
-};
-
-template <int DPL>
-__device__ __forceinline__ Pages load_pages(const int32_t* row, int64_t width, int shift, const Lane<DPL>& L, int key) {
-  // entries past the row's end are not needed: no key lies there
-  const int last = (int)width - 1;
-  Pages p;
-  p.k = row[min((key + 4 * L.c) >> shift, last)];
-#pragma unroll
-  for (int h = 0; h < 2; ++h) p.v[h] = row[min((key + 32 * h + 8 * L.g) >> shift, last)];
-  return p;
-}
-
-template <int DPL>
-__device__ __forceinline__ void load_step(Step<DPL>& s, const KvView& c, int kvh, const Pages& p, const Lane<DPL>& L, int key) {
-  const int mask = c.page() - 1, half = c.dim / 2;
-  const int64_t n = c.n_pages;
-  {
-    const int64_t page = (uint32_t)p.k < (uint32_t)n ? p.k : 0;  // another page's keys are not seen
-    const int off = (key + 4 * L.c) & mask;
-    const uint8_t* const codes = c.K + c.code_at(page, kvh) + (int64_t)off * half;
-    const uint8_t* const scales = c.Ks + c.scale_at(page, kvh) + off;
-#pragma unroll
-    for (int x = 0; x < Step<DPL>::DC; ++x) {
-      const uint8_t* const at = codes + L.kblk[x] * 16;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) s.k[x][j] = *reinterpret_cast<const u32x4*>(at + j * half);
-      s.ks[x] = *reinterpret_cast<const uint32_t*>(scales + ((int64_t)L.kblk[x] << c.page_shift));
-    }
-  }
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int64_t page = (uint32_t)p.v[h] < (uint32_t)n ? p.v[h] : 0;
-    const int off = (key + 32 * h + 8 * L.g) & mask;
-    const uint8_t* const at = c.V + c.code_at(page, kvh) + (int64_t)off * half + L.vd / 2;
-#pragma unroll
-    for (int u = 0; u < 8; ++u) s.v[h][u] = *reinterpret_cast<const typename VWord<DPL>::type*>(at + u * half);
-    s.vs[h] = *reinterpret_cast<const u32x2*>(c.Vs + c.scale_at(page, kvh) + ((int64_t)(L.vd / kKvBlock) << c.page_shift) + off);
-  }
-}
-
-template <int SEL>
-__device__ __forceinline__ uint32_t two_values(uint32_t w, float scale) {
-  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, SEL));
-}
-
-// Elements 2 B, 2 B + 1 of eight tokens as two operands of eight bf16 values each
-template <int B>
-__device__ __forceinline__ void two_operands(const uint32_t (&w)[8], const float (&scale)[8], bf16x8& even, bf16x8& odd) {
-  u32x4 e, o;
-#pragma unroll
-  for (int u = 0; u < 4; ++u) {
-    const uint32_t a = two_values<B>(w[2 * u], scale[2 * u]), b = two_values<B>(w[2 * u + 1], scale[2 * u + 1]);
-    e[u] = __builtin_amdgcn_perm(b, a, 0x05040100u);
-    o[u] = __builtin_amdgcn_perm(b, a, 0x07060302u);
-  }
-  even = __builtin_bit_cast(bf16x8, e);
-  odd = __builtin_bit_cast(bf16x8, o);
-}
-
 template <int DPL>
 __device__ __forceinline__ uint32_t word_of(const typename VWord<DPL>::type& v, int i) {
   if constexpr (DPL == 16) return v[i];
   else return v;
 }
 
-// Queries as the first operand of the scores, in QT bf16 terms: one is a bf16 query itself, three leave 2^-24 of an fp32 element.
-// Keys are converted to bf16 (exact).  The matrix unit would take them as they are held, against 8-bit terms of the
-// queries, at the same rate; but its sums of 8-bit products keep only 2^-17 of their terms at worst (7e-7 on the average), these 2^-23.
-template <int QT, int DC>
-struct Query {
-  bf16x8 q[DC][QT][4];
-  template <class X>
-  __device__ __forceinline__ void load(const typename X::storage* row, int D, bool real, bool wide, int g) {
+template <int SEL>
+__device__ __forceinline__ uint32_t two_values(uint32_t w, float scale) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, SEL));
+}
+__device__ __forceinline__ bf16x8 eight_values(uint32_t w, float scale) {
+  return __builtin_bit_cast(bf16x8, u32x4{two_values<0>(w, scale), two_values<1>(w, scale), two_values<2>(w, scale), two_values<3>(w, scale)});
+}
+
+// Lane (c, g) of a wave: of a key, the 8 KW elements from 8 KW g on, of token 4 c + j; of a value, the DPL elements from DPL c on, of the tokens 16 g ..
+template <int DPL>
+struct Lane {
+  static constexpr int KW = DPL / 2, KB = KW == 8 ? 2 : 1;  // words of a key; blocks that they lie in
+  int c, g;
+  int kd[KB];  // first element of its block's part (in range: what lies past the head's end meets queries of zero)
+  bool kin[KB];
+  int vd;      // first element of its values (in range: such columns are not stored)
+  __device__ __forceinline__ Lane(int dim) {
+    const int lane = threadIdx.x % kWave;
+    c = lane % 16;
+    g = lane / 16;
 #pragma unroll
-    for (int x = 0; x < DC; ++x)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int d = 128 * x + 32 * g + 16 * h;
-        float e[16];
-        load_q16<X>(row, d, real && d < D, wide, e);
-#pragma unroll
-        for (int t = 0; t < QT; ++t)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const __bf16 v = (__bf16)e[i];
-            q[x][t][2 * h + i / 8][i % 8] = v;
-            if (t + 1 < QT) e[i] -= (float)v;
-          }
-      }
-  }
-  // s[j] += scores of tokens 4 c + j over the x-th 128 elements
-  __device__ __forceinline__ void times(int x, const u32x4 (&k)[4], uint32_t ks, f32x4 (&s)[4]) const {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float sc = scale_value((ks >> (8 * j)) & 255u);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const u32x4 w = {two_values<0>(k[j][i], sc), two_values<1>(k[j][i], sc), two_values<2>(k[j][i], sc), two_values<3>(k[j][i], sc)};
-#pragma unroll
-        for (int t = 0; t < QT; ++t) s[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[x][t][i], __builtin_bit_cast(bf16x8, w), s[j], 0, 0, 0);
-      }
+    for (int x = 0; x < KB; ++x) {
+      const int d = 8 * KW * g + kKvBlock * x;
+      kin[x] = d < dim;
+      kd[x] = kin[x] ? d : 0;
     }
+    vd = c * DPL < dim ? c * DPL : 0;
   }
 };
 
-// One launch for every cut of the work: a workgroup takes an equal share of the units, whichever tiles they belong to.
-template <class X, int NR, int DPL>
-__global__ __launch_bounds__(kThreads, DPL == 16 ? 1 : 2) void few_kernel(Few f) {
+template <int DPL>
+struct Keys {
+  uint32_t w[4][Lane<DPL>::KW];
+  uint32_t scale[Lane<DPL>::KB];  // of the four tokens, a byte each
+};
+template <int DPL>
+struct Values {
+  typename VWord<DPL>::type w[16];
+  u32x4 scale;
+};
+
+// a request's row of the table, and the head's rows in page 0 with the bytes from page to page (below 2^32: 4096 heads of 128 bytes, 4096 tokens)
+struct Where {
+  const int32_t* row;
+  const uint8_t *K, *Ks, *V, *Vs;
+  uint32_t code_stride, scale_stride;
+};
+__device__ __forceinline__ int page_of(const KvAttend& a, const Where& at, int key) {
+  return at.row[min(key >> a.c.page_shift, (int)a.width - 1)];  // (entries past the row's end: no key lies there)
+}
+__device__ __forceinline__ bool is_page(const KvAttend& a, int page) { return (uint32_t)page < (uint32_t)a.c.n_pages; }
+
+template <int DPL>
+__device__ __forceinline__ void load_keys(Keys<DPL>& k, const KvAttend& a, const Where& at, int page, const Lane<DPL>& L, int key, int half) {
+  const KvView& c = a.c;
+  const uint32_t p = is_page(a, page) ? page : 0;  // another page's keys: they are not seen
+  const int off = (key + 4 * L.c) & (c.page() - 1);
+  const uint8_t* const codes = at.K + (uint64_t)p * at.code_stride + off * half;
+  const uint8_t* const scales = at.Ks + (uint64_t)p * at.scale_stride + off;
+#pragma unroll
+  for (int x = 0; x < Lane<DPL>::KB; ++x) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint8_t* const from = codes + j * half + L.kd[x] / 2;
+      if constexpr (DPL == 4) {
+        const u32x2 v = *reinterpret_cast<const u32x2*>(from);
+        k.w[j][0] = v[0];
+        k.w[j][1] = v[1];
+      } else {
+        const u32x4 v = *reinterpret_cast<const u32x4*>(from);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) k.w[j][4 * x + i] = v[i];
+      }
+    }
+    k.scale[x] = *reinterpret_cast<const uint32_t*>(scales + ((L.kd[x] / kKvBlock) << c.page_shift));
+  }
+}
+template <int DPL>
+__device__ __forceinline__ void load_values(Values<DPL>& v, const KvAttend& a, const Where& at, int page, const Lane<DPL>& L, int key, int half) {
+  const KvView& c = a.c;
+  const uint32_t p = is_page(a, page) ? page : 0;
+  const int off = (key + 16 * L.g) & (c.page() - 1);
+  const uint8_t* const from = at.V + (uint64_t)p * at.code_stride + (off * half + L.vd / 2);
+#pragma unroll
+  for (int u = 0; u < 16; ++u) v.w[u] = *reinterpret_cast<const typename VWord<DPL>::type*>(from + u * half);
+  v.scale = *reinterpret_cast<const u32x4*>(at.Vs + (uint64_t)p * at.scale_stride + (((L.vd / kKvBlock) << c.page_shift) + off));
+}
+
+// Rows of the products.  Rows r of a tile lie in lane group r % 4 and register r / 4 of the scores.  FOLD: two rows of fp32, whose three terms (of a
+// query, of a weight) are rows of one product instead of three products: row r's terms are the registers of lane group r of the scores,
+// which are added, and the registers of lane groups 2 r and 2 r + 1 (even, odd elements) of the output, which are added at the end.
+template <bool F, int NR>
+struct Rows {
+  static constexpr bool kFold = F && NR == 0;
+  static constexpr int kTile = kFold ? 2 : 4 * NR;      // rows of a tile
+  static constexpr int kRegs = kFold ? 1 : NR;          // registers of scores
+  static constexpr int kChain = F && !kFold ? 3 : 1;    // products that add up terms
+  static constexpr int kImages = F ? 3 : 1;             // of the weights in LDS
+  static constexpr int kOut = kRegs > 2 ? 2 : 1;        // products that share converted values
+  // row of the tile, and term, that row x of the first product has (-1: none)
+  __device__ static __forceinline__ int row(int x) { return kFold ? (x / 4 < 2 && x % 4 < 3 ? x / 4 : -1) : (x % 4 < NR ? x / 4 + 4 * (x % 4) : -1); }
+  __device__ static __forceinline__ int term(int x) { return kFold ? min(x % 4, 2) : 0; }
+};
+
+template <class X, int NR, int DPL, bool EXACT>
+__global__ __launch_bounds__(kThreads, DPL == 16 || NR > 1 ? 2 : 3) void few_kernel(Few f) {
   constexpr bool F = sizeof(typename X::storage) == 4;
-  constexpr int QT = F ? 3 : 1, PT = F ? 3 : 1, DC = Step<DPL>::DC, TR = 4 * NR;
-  __shared__ int64_t scan[8];
-  __shared__ alignas(16) uint16_t weights[kWaves][PT][kRows][kPStride];
-  __shared__ alignas(16) float sums[2][4 * NR][16 * DPL];
-  __shared__ float stats[kWaves][2][4 * NR];
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  using R = Rows<F, NR>;
+  using Ln = Lane<DPL>;
+  constexpr int KW = Ln::KW, KB = Ln::KB, TR = R::kTile, NS = R::kRegs, CH = R::kChain, NO = R::kOut, JP = DPL / 2;
+  __shared__ Prefix prefix;
+  __shared__ alignas(16) uint16_t weights[kWaves][R::kImages][TR][kPStride];
+  __shared__ alignas(16) float sums[2][TR][16 * DPL];
+  __shared__ float stats[kWaves][2][TR];
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const KvAttend& a = f.a;
-  const int D = a.c.dim;
-  const Lane<DPL> L(D);
+  const int D = EXACT ? 16 * DPL : a.c.dim;
+  const Ln L(D);
 
   // tokens of no request
   {
@@ -259,146 +249,273 @@ __global__ __launch_bounds__(kThreads, DPL == 16 ? 1 : 2) void few_kernel(Few f)
       for (int64_t i = t0 * a.heads + me; i < a.T * a.heads; i += all) a.lse[i] = -INFINITY;
   }
 
-  const int64_t total = total_units(f, scan);
-  const int64_t W = min((int64_t)gridDim.x, total), w = blockIdx.x;  // every workgroup that takes part has a unit
-  if (threadIdx.x == 0) f.heads[4 * w] = -1;
-  if (w >= W) return;
-  int64_t u = total * w / W;
-  const int64_t u_end = total * (w + 1) / W;
-  Place at = place_of_unit(f, u, scan);
-  int b = at.b;
-  int64_t before = at.before;
-
-  for (int i = threadIdx.x; i < kWaves * PT * kRows * kPStride / 2; i += kThreads) reinterpret_cast<uint32_t*>(weights)[i] = 0;
-  __syncthreads();
+  // this wave's units
+  const int64_t me = (int64_t)blockIdx.x * kWaves + wave;
+  if (!f.whole && threadIdx.x < kWaves) f.cuts[4 * (blockIdx.x * kWaves + threadIdx.x)] = -1;
+  int64_t total = scan_requests(f, 0, prefix);
+  for (int64_t b0 = kThreads; b0 < a.B; b0 += kThreads) total += scan_requests(f, b0, prefix);
+  if (total == 0) return;
+  const Shares sh = shares_of(total, gridDim.x);
+  int64_t u, u_end;
+  if (f.whole) {
+    u = blockIdx.x;
+    u_end = total;
+  } else {
+    if (blockIdx.x >= sh.groups) return;
+    u = sh.first_unit(me);
+    u_end = sh.first_unit(me + 1);
+  }
+  int b = 0;
+  int64_t before = 0;
+  {
+    // the request of unit u
+    int64_t carry = 0;
+    bool found = false;
+    for (int64_t b0 = 0; b0 < a.B && carry < total; b0 += kThreads) {
+      const int64_t here = a.B <= kThreads ? total : scan_requests(f, b0, prefix);
+      if (!found && u < carry + here) {
+        int lo = 0, hi = kThreads - 1;  // the first request whose inclusive sum is above u - carry
+        while (lo < hi) {
+          const int mid = (lo + hi) >> 1;
+          if (prefix.incl[mid] > u - carry) hi = mid;
+          else lo = mid + 1;
+        }
+        b = (int)b0 + lo;
+        before = carry + (lo ? prefix.incl[lo - 1] : 0);
+        found = true;
+      }
+      carry += here;
+    }
+    b = __builtin_amdgcn_readfirstlane(b);
+  }
+  // whether the workgroup's units are all steps of one tile: its waves' parts are then joined here
+  bool together = f.whole;
+  if (!f.whole) {
+    if (threadIdx.x == 0) {
+      const Steps st = steps_of(f, span_at(f, prefix, b));
+      const int64_t per = tile_units(f, st), g0 = sh.of_group(blockIdx.x) - before, g1 = sh.of_group(blockIdx.x + 1) - before;
+      const int64_t tile = divide(g0, per);
+      stats[0][0][0] = total >= kWaves && g0 >= tile * per + (g0 > tile * per ? kTileCost : 0) && g1 <= (tile + 1) * per && g1 - g0 >= kWaves * (kTileCost + 1) ? 1.f : 0.f;
+    }
+    __syncthreads();
+    together = stats[0][0][0] != 0.f;
+    __syncthreads();
+    if (threadIdx.x == 0) f.joined[blockIdx.x] = together;
+  }
 
   const float zscale = a.scale * kLog2e;
+  // row of the output product: the weights' image and row that lane c's row has, and whether it is the one of the odd elements
+  int p_row[NO];
+  bool p_odd;
+  if constexpr (R::kFold) {
+    p_row[0] = (min(L.c % 4, 2) * TR + L.c / 8) * kPStride;
+    p_odd = (L.c / 4) & 1;
+  } else {
+#pragma unroll
+    for (int y = 0; y < NO; ++y) p_row[y] = (L.c / 4 + 4 * min(2 * y + (L.c % 4) / 2, NS - 1)) * kPStride;
+    p_odd = L.c & 1;
+  }
+  const uint32_t sel0 = p_odd ? 0x01000c0cu : 0x0c0c0100u, sel1 = p_odd ? 0x03020c0cu : 0x0c0c0302u;
+  uint16_t* const my_weights = &weights[wave][0][0][0];
+  constexpr int kImage = TR * kPStride;
+
   while (u < u_end) {
-    Span sp = span_of(a, b);
-    int per, tiles;
-    int64_t mine = units_of(f, sp, per, tiles);
+    Span sp = span_at(f, prefix, b);
+    Steps st = steps_of(f, sp);
+    int per = tile_units(f, st);
+    int64_t mine = (int64_t)st.tiles * a.c.heads * per;
     while (u >= before + mine) {  // the next request with rows
       before += mine;
       ++b;
-      sp = span_of(a, b);
-      mine = units_of(f, sp, per, tiles);
+      sp = span_at(f, prefix, b);
+      st = steps_of(f, sp);
+      per = tile_units(f, st);
+      mine = (int64_t)st.tiles * a.c.heads * per;
     }
-    const int seg = (int)((u - before) / per), first = (int)(u - before - (int64_t)seg * per);
-    const int64_t seg_begin = before + (int64_t)seg * per, seg_end = seg_begin + per;
-    const int last = (int)(min(u_end, seg_end) - seg_begin);
-    const int kvh = seg % a.c.heads, tile = seg / a.c.heads;
+    sp.t0 = __builtin_amdgcn_readfirstlane(sp.t0);
+    sp.n = __builtin_amdgcn_readfirstlane(sp.n);
+    sp.len = __builtin_amdgcn_readfirstlane(sp.len);
+    const int seg = __builtin_amdgcn_readfirstlane((int)divide(u - before, per));
+    const int64_t seg_begin = before + (int64_t)seg * per;
+    const int tile = (int)((uint32_t)seg / (uint32_t)a.c.heads), kvh = seg - tile * a.c.heads;
     const int rows = min(TR, sp.n * f.group - tile * TR);
+    int first, last;  // steps
+    if (f.whole) {
+      first = st.per_tile * wave / kWaves;
+      last = st.per_tile * (wave + 1) / kWaves;
+    } else {
+      first = max(0, (int)(u - seg_begin) - kTileCost);
+      last = (int)(min(u_end, seg_begin + per) - seg_begin) - kTileCost;
+      if (last <= 0 && !together) {  // the tile begins with the next wave
+        u = u_end;
+        break;
+      }
+    }
+    first = __builtin_amdgcn_readfirstlane(first);
+    last = __builtin_amdgcn_readfirstlane(last);
 
-    // row r of the tile is row 4 (r % 4) + r / 4 of the products: up to four rows lie in one accumulator register of the four lane groups
-    Query<QT, DC> q;
+    const int64_t code0 = a.c.code_at(0, kvh), scale0 = a.c.scale_at(0, kvh);
+    const Where at{a.table + (int64_t)b * a.width, a.c.K + code0, a.c.Ks + scale0, a.c.V + code0, a.c.Vs + scale0,
+                   (uint32_t)a.c.code_at(1, 0), (uint32_t)a.c.scale_at(1, 0)};
+    const int key_end = min(sp.len, last * kStep);
+    int key = first * kStep;
+    Keys<DPL> K;
+    Values<DPL> V;
+    int pk = 0, pv = 0, pk1 = 0, pv1 = 0;  // page ids of the lane's keys and values: of this step and the next
+    if (key < key_end) {
+      pk = page_of(a, at, key + 4 * L.c);
+      pv = page_of(a, at, key + 16 * L.g);
+      pk1 = page_of(a, at, key + kStep + 4 * L.c);
+      pv1 = page_of(a, at, key + kStep + 16 * L.g);
+      load_keys<DPL>(K, a, at, pk, L, key, D / 2);
+      load_values<DPL>(V, a, at, pv, L, key, D / 2);
+    }
+
+    bf16x8 q[CH][KW];
     {
-      const int r = (L.c >> 2) + 4 * (L.c & 3), rid = tile * TR + r;
-      const bool real = r < rows;
+      const int r = R::row(L.c), rid = tile * TR + r;
+      const bool real = r >= 0 && r < rows;
       const int tok = real ? rid / f.group : 0, head = kvh * f.group + (real ? rid % f.group : 0);
-      q.template load<X>(reinterpret_cast<const typename X::storage*>(a.Q) + (int64_t)(sp.t0 + tok) * a.q_stride + (int64_t)head * D, D, real, f.q_wide, L.g);
-    }
-    // the last key that a row sees: rows r = g + 4 i of this lane
-    int lim[NR];
-    int lim_low = sp.len - 1;
+      const typename X::storage* const Q = reinterpret_cast<const typename X::storage*>(a.Q) + (int64_t)(sp.t0 + tok) * a.q_stride + (int64_t)head * D;
 #pragma unroll
-    for (int i = 0; i < NR; ++i) {
-      const int r = L.g + 4 * i, tok = (tile * TR + r) / f.group;
-      lim[i] = r < rows ? sp.len - sp.n + tok : -1;
+      for (int x = 0; x < KW / 2; ++x) {
+        float e[16];
+        const int d = 8 * KW * L.g + 16 * x;
+        load_q16<X>(Q, d, real && d < D, f.q_wide, e);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          if constexpr (R::kFold) {
+            const float h = (float)(__bf16)e[i], m = (float)(__bf16)(e[i] - h);
+            const int t = R::term(L.c);
+            q[0][2 * x + i / 8][i % 8] = (__bf16)(t == 0 ? e[i] : t == 1 ? e[i] - h : e[i] - h - m);
+          } else {
+#pragma unroll
+            for (int t = 0; t < CH; ++t) {
+              const __bf16 v = (__bf16)e[i];
+              q[t][2 * x + i / 8][i % 8] = v;
+              if (t + 1 < CH) e[i] -= (float)v;
+            }
+          }
+        }
+      }
     }
-    lim_low = sp.len - sp.n + (tile * TR) / f.group;  // what every row of the tile sees
+    // the last key that a row sees: by the layout of the scores, and of the output (the same but where terms are folded)
+    int lim[NS], lim_o[NS];
+    const auto last_key = [&](int r) { return r < rows ? sp.len - sp.n + (tile * TR + r) / f.group : -1; };
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      lim[i] = last_key(L.g + 4 * i);
+      lim_o[i] = R::kFold ? last_key(L.g / 2) : lim[i];
+    }
+    const int lim_low = sp.len - sp.n + tile * TR / f.group;  // what every row of the tile sees
 
-    f32x4 o[DPL];
-    float m[NR], l[NR];
+    f32x4 o[NO][JP];
+    float m[NS], l[NS];
 #pragma unroll
-    for (int j = 0; j < DPL; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int y = 0; y < NO; ++y)
 #pragma unroll
-    for (int i = 0; i < NR; ++i) {
+      for (int j = 0; j < JP; ++j) o[y][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
       m[i] = -INFINITY;
       l[i] = 0.f;
     }
-
-    const int32_t* const trow = a.table + (int64_t)b * a.width;
-    const int key_end = min(sp.len, last * kUnit);
-    int key = first * kUnit + wave * kStep;
-    Step<DPL> cur, nxt;
-    Pages pc, pn;
-    if (key < key_end) {
-      pc = load_pages<DPL>(trow, a.width, a.c.page_shift, L, key);
-      pn = load_pages<DPL>(trow, a.width, a.c.page_shift, L, key + kUnit);
-      load_step<DPL>(cur, a.c, kvh, pc, L, key);
-    }
-    while (key < key_end) {
-      const bool more = key + kUnit < key_end;
-      Pages p2 = pn;
-      if (more) {
-        load_step<DPL>(nxt, a.c, kvh, pn, L, key + kUnit);
-        p2 = load_pages<DPL>(trow, a.width, a.c.page_shift, L, key + 2 * kUnit);
+    const auto scale_out = [&](const float (&by)[NS]) {  // by: of the lane's rows of scores
+      if constexpr (R::kFold) {
+        const float k = __shfl(by[0], (L.g / 2) * 16 + L.c, kWave);
+#pragma unroll
+        for (int j = 0; j < JP; ++j) o[0][j] *= k;
+      } else {
+#pragma unroll
+        for (int i = 0; i < NS; ++i)
+#pragma unroll
+          for (int j = 0; j < JP; ++j) {
+            o[i / 2][j][2 * (i % 2)] *= by[i];
+            o[i / 2][j][2 * (i % 2) + 1] *= by[i];
+          }
       }
+    };
+
+    while (key < key_end) {
+      const bool more = key + kStep < key_end;
       // scores: rows by tokens 4 c + j
       f32x4 s[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) s[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int j = 0; j < 4; ++j) {
+        s[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int x = 0; x < DC; ++x) q.times(x, cur.k[x], L.kreal[x] ? cur.ks[x] : 0x7f7f7f7fu, s);  // (queries are zero past the head's end)
-      float z[NR][4];
+        for (int w = 0; w < KW; ++w) {
+          const int x = w / 4 < KB ? w / 4 : 0;
+          const float sc = L.kin[x] ? scale_value((K.scale[x] >> (8 * j)) & 255u) : 1.f;
+          const bf16x8 k = eight_values(K.w[j][w], sc);
 #pragma unroll
-      for (int i = 0; i < NR; ++i)
+          for (int t = 0; t < CH; ++t) s[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[t][w], k, s[j], 0, 0, 0);
+        }
+      }
+      const bool k_there = is_page(a, pk), v_there = is_page(a, pv);
+      if (more) {
+        pk = pk1;
+        load_keys<DPL>(K, a, at, pk, L, key + kStep, D / 2);
+        pk1 = page_of(a, at, key + 2 * kStep + 4 * L.c);
+      }
+      float z[NS][4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) z[i][j] = s[j][i] * zscale;
-      const uint32_t np = (uint32_t)a.c.n_pages;
-      const bool k_there = (uint32_t)pc.k < np;
-      bool v_there[2];
+      for (int i = 0; i < NS; ++i)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) v_there[h] = (uint32_t)pc.v[h] < np;
-      if (key + kStep - 1 > lim_low || __any(!k_there || !v_there[0] || !v_there[1])) {
+        for (int j = 0; j < 4; ++j) z[i][j] = (R::kFold ? s[j][0] + s[j][1] + s[j][2] : s[j][i]) * zscale;
+      if (key + kStep - 1 > lim_low || __any(!k_there || !v_there)) {
         // the end of the keys, keys that only some rows see, or pages that are not there
         int bad = 0x7fffffff;
 #pragma unroll
-        for (int i = 0; i < NR; ++i)
+        for (int i = 0; i < NS; ++i)
 #pragma unroll
           for (int j = 0; j < 4; ++j) z[i][j] = k_there && key + 4 * L.c + j <= lim[i] ? z[i][j] : -INFINITY;
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int x = 0; x < 8; ++x) {
-            // a value that no row sees, or that is NaN, does not enter the product: 0 times it would not be 0
-            const int k = key + 32 * h + 8 * L.g + x, sh = 8 * (x & 3);
-            const bool seen = v_there[h] && k < sp.len, nan = ((cur.vs[h][x / 4] >> sh) & 255u) == 255u;
-            if (seen && nan) bad = min(bad, k);
-            if (!seen || nan) {
-              cur.v[h][x] = typename VWord<DPL>::type{};
-              cur.vs[h][x / 4] = (cur.vs[h][x / 4] & ~(255u << sh)) | (127u << sh);
-            }
+        for (int x = 0; x < 16; ++x) {
+          // a value that no row sees, or that is NaN, does not enter the product: 0 times it would not be 0
+          const int k = key + 16 * L.g + x, shift = 8 * (x & 3);
+          const bool seen = v_there && k < sp.len, nan = ((V.scale[x / 4] >> shift) & 255u) == 255u;
+          if (seen && nan) bad = min(bad, k);
+          if (!seen || nan) {
+            V.w[x] = typename VWord<DPL>::type{};
+            V.scale[x / 4] = (V.scale[x / 4] & ~(255u << shift)) | (127u << shift);
           }
+        }
         // ... it goes to the rows that see it, in the elements of its block
         bad = min(bad, __shfl_xor(bad, 16, kWave));
         bad = min(bad, __shfl_xor(bad, 32, kWave));
 #pragma unroll
-        for (int i = 0; i < NR; ++i)
-          if (bad <= lim[i]) {
+        for (int i = 0; i < NS; ++i)
+          if (bad <= lim_o[i]) {
 #pragma unroll
-            for (int j = 0; j < DPL; ++j) o[j][i] = NAN;
+            for (int j = 0; j < JP; ++j) {
+              if constexpr (R::kFold) o[0][j][0] = NAN;
+              else o[i / 2][j][2 * (i % 2)] = o[i / 2][j][2 * (i % 2) + 1] = NAN;
+            }
           }
       }
       // the maximum
       bool moves = false;
+      float top[NS];
 #pragma unroll
-      for (int i = 0; i < NR; ++i) moves |= fmaxf(fmaxf(z[i][0], z[i][1]), fmaxf(z[i][2], z[i][3])) > m[i] + kSlack;
+      for (int i = 0; i < NS; ++i) {
+        top[i] = fmaxf(fmaxf(z[i][0], z[i][1]), fmaxf(z[i][2], z[i][3]));
+        moves |= top[i] > m[i] + kSlack;
+      }
       if (__any(moves)) {
+        float keep[NS];
 #pragma unroll
-        for (int i = 0; i < NR; ++i) {
-          const float top = row16_max(fmaxf(fmaxf(z[i][0], z[i][1]), fmaxf(z[i][2], z[i][3])));
-          const float next = fmaxf(m[i], top);
-          const float keep = next == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[i] - next);
+        for (int i = 0; i < NS; ++i) {
+          const float next = fmaxf(m[i], row16_max(top[i]));
+          keep[i] = next == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[i] - next);
           m[i] = next;
-          l[i] *= keep;
-#pragma unroll
-          for (int j = 0; j < DPL; ++j) o[j][i] *= keep;
+          l[i] *= keep[i];
         }
+        scale_out(keep);
       }
       // weights, through LDS into the layout of the second product
 #pragma unroll
-      for (int i = 0; i < NR; ++i) {
+      for (int i = 0; i < NS; ++i) {
         const float base = m[i] == -INFINITY ? 0.f : m[i];
         float p[4];
 #pragma unroll
@@ -407,42 +524,46 @@ __global__ __launch_bounds__(kThreads, DPL == 16 ? 1 : 2) void few_kernel(Few f)
           l[i] += p[j];
         }
 #pragma unroll
-        for (int t = 0; t < PT; ++t) {
-          u32x2 pk;
+        for (int t = 0; t < R::kImages; ++t) {
+          u32x2 pair;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const bf16x2 v = {(__bf16)p[2 * h], (__bf16)p[2 * h + 1]};
-            pk[h] = __builtin_bit_cast(uint32_t, v);
-            if (t + 1 < PT) {
-              p[2 * h] -= bf16_lo(pk[h]);
-              p[2 * h + 1] -= bf16_hi(pk[h]);
+          for (int y = 0; y < 2; ++y) {
+            const bf16x2 v = {(__bf16)p[2 * y], (__bf16)p[2 * y + 1]};
+            pair[y] = __builtin_bit_cast(uint32_t, v);
+            if (t + 1 < R::kImages) {
+              p[2 * y] -= bf16_lo(pair[y]);
+              p[2 * y + 1] -= bf16_hi(pair[y]);
             }
           }
-          *reinterpret_cast<u32x2*>(&weights[wave][t][4 * L.g + i][4 * L.c]) = pk;
+          if (!R::kFold || L.g < TR) *reinterpret_cast<u32x2*>(my_weights + t * kImage + (L.g + 4 * i) * kPStride + 4 * L.c) = pair;
         }
       }
       order_lds();
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        bf16x8 pa[PT];
+      for (int y4 = 0; y4 < 4; ++y4) {  // tokens 16 g + 4 y4 ..
+        bf16x8 p[NO][CH];
 #pragma unroll
-        for (int t = 0; t < PT; ++t) pa[t] = *reinterpret_cast<const bf16x8*>(&weights[wave][t][L.c][32 * h + 8 * L.g]);
-        float vsc[8];
+        for (int y = 0; y < NO; ++y)
 #pragma unroll
-        for (int x = 0; x < 8; ++x) vsc[x] = scale_value((cur.vs[h][x / 4] >> (8 * (x & 3))) & 255u);
+          for (int t = 0; t < CH; ++t) {
+            const u32x2 w = *reinterpret_cast<const u32x2*>(my_weights + t * kImage + p_row[y] + 16 * L.g + 4 * y4);
+            p[y][t] = __builtin_bit_cast(bf16x8, u32x4{__builtin_amdgcn_perm(w[0], w[0], sel0), __builtin_amdgcn_perm(w[0], w[0], sel1),
+                                                       __builtin_amdgcn_perm(w[1], w[1], sel0), __builtin_amdgcn_perm(w[1], w[1], sel1)});
+          }
+        float sc[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) sc[x] = scale_value((V.scale[y4] >> (8 * x)) & 255u);
 #pragma unroll
         for (int i = 0; i < (DPL + 7) / 8; ++i) {
-          uint32_t word[8];
+          uint32_t w[4];
 #pragma unroll
-          for (int x = 0; x < 8; ++x) word[x] = word_of<DPL>(cur.v[h][x], i);
-#define GSI_VALUES(B)                                                                                          \
-  {                                                                                                            \
-    bf16x8 even, odd;                                                                                          \
-    two_operands<B>(word, vsc, even, odd);                                                                     \
-    _Pragma("unroll") for (int t = 0; t < PT; ++t) {                                                           \
-      o[8 * i + 2 * B] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pa[t], even, o[8 * i + 2 * B], 0, 0, 0);      \
-      o[8 * i + 2 * B + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pa[t], odd, o[8 * i + 2 * B + 1], 0, 0, 0); \
-    }                                                                                                          \
+          for (int x = 0; x < 4; ++x) w[x] = word_of<DPL>(V.w[4 * y4 + x], i);
+#define GSI_VALUES(B)                                                                                                                   \
+  {                                                                                                                                     \
+    const bf16x8 v = __builtin_bit_cast(bf16x8, u32x4{two_values<B>(w[0], sc[0]), two_values<B>(w[1], sc[1]), two_values<B>(w[2], sc[2]), \
+                                                      two_values<B>(w[3], sc[3])});                                                     \
+    _Pragma("unroll") for (int y = 0; y < NO; ++y) _Pragma("unroll") for (int t = 0; t < CH; ++t)                                       \
+        o[y][4 * i + B] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p[y][t], v, o[y][4 * i + B], 0, 0, 0);                                \
   }
           GSI_VALUES(0)
           GSI_VALUES(1)
@@ -454,178 +575,299 @@ __global__ __launch_bounds__(kThreads, DPL == 16 ? 1 : 2) void few_kernel(Few f)
         }
       }
       order_lds();
-      cur = nxt;
-      pc = pn;
-      pn = p2;
-      key += kUnit;
+      if (more) {
+        pv = pv1;
+        load_values<DPL>(V, a, at, pv, L, key + kStep, D / 2);
+        pv1 = page_of(a, at, key + 2 * kStep + 16 * L.g);
+      }
+      key += kStep;
     }
 
-    // the four waves' sums, in a fixed order: 2 onto 0 and 3 onto 1, then 1 onto 0
-    float scale_o[NR], top[NR], sum[NR];
+    // the row's sums: o of element pairs (2 j, 2 j + 1) of the lane's DPL elements, from here on element by element in `out`
+    float out[NS][DPL];
 #pragma unroll
-    for (int i = 0; i < NR; ++i) {
-      l[i] = row16_sum(l[i]);
-      if (L.c == 0) {
-        stats[wave][0][4 * i + L.g] = m[i];
-        stats[wave][1][4 * i + L.g] = l[i];
+    for (int i = 0; i < NS; ++i) l[i] = row16_sum(l[i]);
+    if constexpr (R::kFold) {
+      // even elements lie in lane group 2 r, odd ones in 2 r + 1; lane group r takes both (groups 2 and 3: nothing)
+      const int even = (2 * (L.g & 1)) * 16 + L.c;
+#pragma unroll
+      for (int j = 0; j < JP; ++j) {
+        const float x = o[0][j][0] + o[0][j][1] + o[0][j][2];
+        out[0][2 * j] = __shfl(x, even, kWave);
+        out[0][2 * j + 1] = __shfl(x, even + 16, kWave);
       }
-    }
-    __syncthreads();
+    } else {
 #pragma unroll
-    for (int i = 0; i < NR; ++i) {
-      const int r = 4 * i + L.g;
-      top[i] = -INFINITY;
-      sum[i] = 0.f;
+      for (int i = 0; i < NS; ++i)
 #pragma unroll
-      for (int v = 0; v < kWaves; ++v) top[i] = fmaxf(top[i], stats[v][0][r]);
-#pragma unroll
-      for (int v = 0; v < kWaves; ++v) {
-        const float mv = stats[v][0][r];
-        sum[i] += stats[v][1][r] * (mv == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mv - top[i]));  // (sums of such a wave: 0, or NaN)
-      }
-      scale_o[i] = m[i] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[i] - top[i]);
-    }
-#pragma unroll
-    for (int j = 0; j < DPL; ++j)
-#pragma unroll
-      for (int i = 0; i < NR; ++i) o[j][i] *= scale_o[i];
-    const auto put = [&](int slot) {
-#pragma unroll
-      for (int i = 0; i < NR; ++i)
-#pragma unroll
-        for (int j = 0; j < DPL; j += 4)
-          *reinterpret_cast<f32x4*>(&sums[slot][4 * i + L.g][DPL * L.c + j]) = f32x4{o[j][i], o[j + 1][i], o[j + 2][i], o[j + 3][i]};
-    };
-    const auto add = [&](int slot) {
-#pragma unroll
-      for (int i = 0; i < NR; ++i)
-#pragma unroll
-        for (int j = 0; j < DPL; j += 4) {
-          const f32x4 v = *reinterpret_cast<const f32x4*>(&sums[slot][4 * i + L.g][DPL * L.c + j]);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[j + e][i] += v[e];
+        for (int j = 0; j < JP; ++j) {
+          out[i][2 * j] = o[i / 2][j][2 * (i % 2)];
+          out[i][2 * j + 1] = o[i / 2][j][2 * (i % 2) + 1];
         }
-    };
-    if (wave >= 2) put(wave - 2);
-    __syncthreads();
-    if (wave < 2) add(wave);
-    if (wave == 1) put(1);
-    __syncthreads();
-    if (wave == 0) {
-      add(1);
-      const bool whole = first == 0 && last == per;
+    }
+    const bool holds = !R::kFold || L.g < TR;  // lane groups with rows
+    if (together) {
+      // four waves' sums, in a fixed order: 2 onto 0 and 3 onto 1, then 1 onto 0
+      __syncthreads();
+      if (holds && L.c == 0) {
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+          stats[wave][0][4 * i + L.g] = m[i];
+          stats[wave][1][4 * i + L.g] = l[i];
+        }
+      }
+      __syncthreads();
+      const auto put = [&](int slot) {
+        if (holds) {
+#pragma unroll
+          for (int i = 0; i < NS; ++i)
+#pragma unroll
+            for (int j = 0; j < DPL; j += 4)
+              *reinterpret_cast<f32x4*>(&sums[slot][4 * i + L.g][DPL * L.c + j]) = f32x4{out[i][j], out[i][j + 1], out[i][j + 2], out[i][j + 3]};
+        }
+      };
+      const auto add = [&](int slot) {
+        if (holds) {
+#pragma unroll
+          for (int i = 0; i < NS; ++i)
+#pragma unroll
+            for (int j = 0; j < DPL; j += 4) {
+              const f32x4 v = *reinterpret_cast<const f32x4*>(&sums[slot][4 * i + L.g][DPL * L.c + j]);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) out[i][j + e] += v[e];
+            }
+        }
+      };
+#pragma unroll
+      for (int i = 0; i < NS; ++i) {
+        const int r = holds ? 4 * i + L.g : 0;
+        float top = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (int v = 0; v < kWaves; ++v) top = fmaxf(top, stats[v][0][r]);
+#pragma unroll
+        for (int v = 0; v < kWaves; ++v) {
+          const float mv = stats[v][0][r];
+          sum += stats[v][1][r] * (mv == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mv - top));  // (the sum of such a wave: 0, or NaN)
+        }
+        const float k = m[i] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[i] - top);
+#pragma unroll
+        for (int j = 0; j < DPL; ++j) out[i][j] *= k;
+        m[i] = top;
+        l[i] = sum;
+      }
+      if (wave >= 2) put(wave - 2);
+      __syncthreads();
+      if (wave < 2) add(wave);
+      if (wave == 1) put(1);
+      __syncthreads();
+      if (wave == 0) add(1);
+    }
+    if (!together || wave == 0) {
+      const int64_t to = together && !f.whole ? sh.of_group(blockIdx.x + 1) : u_end;  // where this part ends
+      const bool complete = f.whole || (first == 0 && to >= seg_begin + per);
       float* part = nullptr;
-      if (!whole) {
-        // the first tile of a workgroup, if another began it: slot 2 w; else the tile is cut at this workgroup's end
-        const int64_t slot = first != 0 ? 2 * w : 2 * w + 1;
-        part = f.parts + slot * TR * (D + 2);
+      if (!complete) {
+        // place 2 i: a tile that an earlier wave began; place 2 i + 1: one that begins here and ends elsewhere
+        part = f.parts + (2 * me + (first == 0)) * TR * (D + 2);
         if (first == 0 && lane == 0) {
-          // the workgroup with unit seg_end - 1: the largest v with total * v / W <= seg_end - 1
-          int64_t v = (seg_end * W - 1) / total;
-          while (total * (v + 1) / W <= seg_end - 1) ++v;
-          while (total * v / W > seg_end - 1) --v;
-          f.heads[4 * w + 1] = tile;
-          f.heads[4 * w + 2] = kvh;
-          f.heads[4 * w + 3] = (int)v;
-          f.heads[4 * w] = b;
+          int* const cut = f.cuts + 4 * me;
+          cut[1] = tile;
+          cut[2] = kvh;
+          cut[3] = (int)sh.owner(seg_begin + per - 1);
+          cut[0] = b;
         }
       }
 #pragma unroll
-      for (int i = 0; i < NR; ++i) {
+      for (int i = 0; i < NS; ++i) {
         const int r = 4 * i + L.g;
-        if (r >= rows) continue;
+        if (!holds || r >= rows) continue;
         const int rid = tile * TR + r;
         const int64_t orow = (int64_t)(sp.t0 + rid / f.group) * a.heads + kvh * f.group + rid % f.group;
-        if (whole) {
-          const float inv = sum[i] == 0.f ? 0.f : 1.f / sum[i];
-          typename X::storage* const out = reinterpret_cast<typename X::storage*>(a.O) + orow * D + DPL * L.c;
+        if (complete) {
+          const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
+          typename X::storage* const to_o = reinterpret_cast<typename X::storage*>(a.O) + orow * D + DPL * L.c;
           if (DPL * L.c < D)
 #pragma unroll
             for (int j = 0; j < DPL; j += 4) {
               if constexpr (F) {
-                *reinterpret_cast<f32x4*>(out + j) = f32x4{o[j][i] * inv, o[j + 1][i] * inv, o[j + 2][i] * inv, o[j + 3][i] * inv};
+                *reinterpret_cast<f32x4*>(to_o + j) = f32x4{out[i][j] * inv, out[i][j + 1] * inv, out[i][j + 2] * inv, out[i][j + 3] * inv};
               } else {
-                const bf16x2 lo = {(__bf16)(o[j][i] * inv), (__bf16)(o[j + 1][i] * inv)}, hi = {(__bf16)(o[j + 2][i] * inv), (__bf16)(o[j + 3][i] * inv)};
-                *reinterpret_cast<u32x2*>(out + j) = u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+                const bf16x2 lo = {(__bf16)(out[i][j] * inv), (__bf16)(out[i][j + 1] * inv)}, hi = {(__bf16)(out[i][j + 2] * inv), (__bf16)(out[i][j + 3] * inv)};
+                *reinterpret_cast<u32x2*>(to_o + j) = u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
               }
             }
-          if (a.lse && L.c == 0) a.lse[orow] = sum[i] == 0.f ? -INFINITY : (top[i] == -INFINITY ? sum[i] : (top[i] + log2f(sum[i])) * kLn2);
+          if (a.lse && L.c == 0) a.lse[orow] = l[i] == 0.f ? -INFINITY : (m[i] == -INFINITY ? l[i] : (m[i] + log2f(l[i])) * kLn2);
         } else {
           float* const row = part + r * (D + 2);
           if (DPL * L.c < D)
 #pragma unroll
-            for (int j = 0; j < DPL; j += 2) *reinterpret_cast<f32x2*>(row + DPL * L.c + j) = f32x2{o[j][i], o[j + 1][i]};
+            for (int j = 0; j < DPL; j += 2) *reinterpret_cast<f32x2*>(row + DPL * L.c + j) = f32x2{out[i][j], out[i][j + 1]};
           if (L.c == 0) {
-            row[D] = top[i];
-            row[D + 1] = sum[i];
+            row[D] = m[i];
+            row[D + 1] = l[i];
           }
         }
       }
     }
-    u = min(u_end, seg_end);
-    __syncthreads();  // stats and sums are read before the next tile writes them
+    u = f.whole ? u + gridDim.x : min(u_end, seg_begin + per);
   }
 }
 
-// Joins the parts of the tiles that a cut went through: a workgroup per possible cut and row, in the order of the parts.
+// Joins the parts of the tiles that a cut went through, in their order: a workgroup for the cuts that begin in one of few_kernel's and a row, a wave for
+// each of them; one of many parts is taken by the four waves together.  How much each part counts is worked out first, so that the loads
+// of the parts themselves wait for nothing.
+constexpr int kListed = 512;
 template <class X>
-__global__ __launch_bounds__(kKvMaxDim) void join_kernel(Few f) {
+__global__ __launch_bounds__(kThreads) void join_kernel(Few f) {
+  __shared__ float weight[kWaves][kListed];
+  __shared__ int place[kWaves][kListed];
+  __shared__ float lds[kThreads][5];
   const KvAttend& a = f.a;
-  const int w = blockIdx.x, r = blockIdx.y, D = a.c.dim;
-  const int b = f.heads[4 * w];
-  if (b < 0) return;
-  const int tile = f.heads[4 * w + 1], kvh = f.heads[4 * w + 2], end = f.heads[4 * w + 3];
-  const Span sp = span_of(a, b);
-  const int rid = tile * f.tile_rows + r;
-  if (rid >= sp.n * f.group) return;
-  const auto part = [&](int i) { return f.parts + (int64_t)(i == w ? 2 * w + 1 : 2 * i) * f.tile_rows * (D + 2) + r * (D + 2); };
-  float top = -INFINITY;
-  for (int i = w; i <= end; ++i) top = fmaxf(top, part(i)[D]);
-  const int d = threadIdx.x;
-  float sum = 0.f, o = 0.f;
-  for (int i = w; i <= end; ++i) {
-    const float* const p = part(i);
-    const float mv = p[D], k = mv == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mv - top);
-    sum += p[D + 1] * k;
-    if (d < D) o += p[d] * k;
+  const int D = a.c.dim, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int lanes = D <= 64 ? 16 : D <= 128 ? 32 : 64;  // four elements each
+  typedef int i32x4 __attribute__((ext_vector_type(4)));
+  i32x4 cuts[kWaves];
+#pragma unroll
+  for (int k = 0; k < kWaves; ++k) cuts[k] = *reinterpret_cast<const i32x4*>(f.cuts + 4 * (blockIdx.x * kWaves + k));
+#pragma unroll
+  for (int k = 0; k < kWaves; ++k) {
+    const int w = blockIdx.x * kWaves + k, b = cuts[k][0];
+    if (b < 0) continue;
+    const int tile = cuts[k][1], kvh = cuts[k][2], end = cuts[k][3];
+    const bool many = end - w >= kManyParts;
+    if (!many && wave != k) continue;
+    const Span sp = span_of(a, b);
+    const int rows = min(f.tile_rows, sp.n * f.group - tile * f.tile_rows);
+    const int each = kWave / lanes, ways = many ? each * kWaves : each;     // parts at a time
+    const int way = many ? threadIdx.x / lanes : lane / lanes, d = 4 * ((many ? threadIdx.x : lane) % lanes);
+    // where wave i's part lies (none where its workgroup's first wave has it for the four)
+    const auto slot = [&](int i) { return i == w ? 2 * i + 1 : 2 * i; };
+    for (int r = blockIdx.y; r < rows; r += gridDim.y) {
+      const auto part = [&](int s) { return f.parts + ((int64_t)s * f.tile_rows + r) * (D + 2); };
+      float top = -INFINITY, sum = 0.f;
+      f32x4 o = {0.f, 0.f, 0.f, 0.f};
+      // kListed parts at a time; a wave works out the list by itself, the same one in each where four work together
+      for (int i0 = w; i0 <= end; i0 += kListed) {
+        const int i1 = min(end + 1, i0 + kListed);
+        float mine = -INFINITY;
+        int n = 0;
+        for (int i = i0 + lane; i - lane < i1; i += kWave) {
+          const bool has = i < i1 && (i % kWaves == 0 || !f.joined[i / kWaves]);
+          const float m = has ? part(slot(i))[D] : -INFINITY;
+          const uint64_t ballot = __ballot(has);
+          if (has) {
+            const int at = n + __popcll(ballot & ((1ull << lane) - 1));
+            place[wave][at] = slot(i);
+            weight[wave][at] = m;
+          }
+          n += __popcll(ballot);
+          mine = fmaxf(mine, m);
+        }
+#pragma unroll
+        for (int x = kWave / 2; x; x >>= 1) mine = fmaxf(mine, __shfl_xor(mine, x, kWave));
+        const float next = fmaxf(top, mine), keep = next == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top - next);
+        top = next;
+        sum *= keep;
+        o *= keep;
+        order_lds();
+#pragma unroll 8
+        for (int y = way; y < n; y += ways) {
+          const float* const p = part(place[wave][y]);
+          const float mv = weight[wave][y], x = mv == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mv - top);
+          const f32x2 lo = *reinterpret_cast<const f32x2*>(p + min(d, D - 4)), hi = *reinterpret_cast<const f32x2*>(p + min(d, D - 4) + 2);
+          sum += p[D + 1] * x;
+          o[0] += lo[0] * x;
+          o[1] += lo[1] * x;
+          o[2] += hi[0] * x;
+          o[3] += hi[1] * x;
+        }
+        order_lds();
+      }
+      // the ways' sums, in their order
+      if (many) {
+        float* const mine = lds[threadIdx.x];
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mine[e] = o[e];
+        mine[4] = sum;
+        __syncthreads();
+        if ((int)threadIdx.x < lanes)
+          for (int y = 1; y < ways; ++y) {
+            const float* const other = lds[threadIdx.x + y * lanes];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] += other[e];
+            sum += other[4];
+          }
+      } else {
+        for (int y = lanes; y < kWave; y <<= 1) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], y, kWave);
+          sum += __shfl_xor(sum, y, kWave);
+        }
+      }
+      if ((many ? (int)threadIdx.x : lane) < lanes) {
+        const int rid = tile * f.tile_rows + r;
+        const int64_t orow = (int64_t)(sp.t0 + rid / f.group) * a.heads + kvh * f.group + rid % f.group;
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        typename X::storage* const to = reinterpret_cast<typename X::storage*>(a.O) + orow * D + d;
+        if (d < D)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) X::store(to, e, o[e] * inv);
+        if (a.lse && d == 0) a.lse[orow] = sum == 0.f ? -INFINITY : (top == -INFINITY ? sum : (top + log2f(sum)) * kLn2);
+      }
+    }
   }
-  const int64_t orow = (int64_t)(sp.t0 + rid / f.group) * a.heads + kvh * f.group + rid % f.group;
-  if (d < D) X::store(reinterpret_cast<typename X::storage*>(a.O), orow * D + d, sum == 0.f ? 0.f : o / sum);
-  if (a.lse && d == 0) a.lse[orow] = sum == 0.f ? -INFINITY : (top == -INFINITY ? sum : (top + log2f(sum)) * kLn2);
 }
 
-// The smallest tile that holds the rows of the longest request that is expected.
+// The smallest tile that holds the rows of the longest request that is expected: 2 (fp32), 4 (bf16), 8 or 16.
 int few_tile(const KvAttend& a, int64_t few) {
   const int64_t rows = std::min(std::min(a.max_q, a.T) * (a.heads / a.c.heads), few);
-  return rows <= 4 ? 4 : rows <= 8 ? 8 : 16;
+  if (a.dtype == GSI_F32 && rows <= 2) return 2;
+  if (a.dtype == GSI_BF16 && rows <= 4) return 4;
+  return rows <= 8 ? 8 : 16;
 }
+int64_t few_tiles(const KvAttend& a, int tile_rows) {
+  return a.B * ceil_div(std::min(a.max_q, a.T) * (a.heads / a.c.heads), tile_rows) * a.c.heads;
+}
+bool few_whole(const KvAttend& a, int) { return a.max_len <= 512; }
 int few_workgroups(const KvAttend& a, int tile_rows) {
-  const int64_t tiles = ceil_div(std::min(a.max_q, a.T) * (a.heads / a.c.heads), tile_rows);
-  const double units = (double)a.B * tiles * a.c.heads * (double)ceil_div(a.max_len, kUnit);
+  const double tiles = (double)few_tiles(a, tile_rows);
+  if (few_whole(a, tile_rows)) return (int)std::max(1.0, std::min(tiles, 4096.0));
+  const double units = tiles * (double)ceil_div(a.max_len, kStep) / kWaves;
   return (int)std::max(1.0, std::min(units, 768.0));
 }
 
 template <class X, int NR>
 void launch_few(const Few& f, int W, hipStream_t s) {
   const int D = f.a.c.dim;
-  if (D <= 64) few_kernel<X, NR, 4><<<W, kThreads, 0, s>>>(f);
-  else if (D <= 128) few_kernel<X, NR, 8><<<W, kThreads, 0, s>>>(f);
-  else few_kernel<X, NR, 16><<<W, kThreads, 0, s>>>(f);
+  if (D == 64) few_kernel<X, NR, 4, true><<<W, kThreads, 0, s>>>(f);
+  else if (D == 128) few_kernel<X, NR, 8, true><<<W, kThreads, 0, s>>>(f);
+  else if (D == 256) few_kernel<X, NR, 16, true><<<W, kThreads, 0, s>>>(f);
+  else if (D < 64) few_kernel<X, NR, 4, false><<<W, kThreads, 0, s>>>(f);
+  else if (D < 128) few_kernel<X, NR, 8, false><<<W, kThreads, 0, s>>>(f);
+  else few_kernel<X, NR, 16, false><<<W, kThreads, 0, s>>>(f);
 }
 template <class X>
 void launch_few(const Few& f, int W, hipStream_t s) {
-  if (f.tile_rows == 4) launch_few<X, 1>(f, W, s);
+  constexpr int kSmall = sizeof(typename X::storage) == 4 ? 0 : 1;
+  if (f.tile_rows <= 4) launch_few<X, kSmall>(f, W, s);
   else if (f.tile_rows == 8) launch_few<X, 2>(f, W, s);
   else launch_few<X, 4>(f, W, s);
-  join_kernel<X><<<dim3(W, f.tile_rows), kKvMaxDim, 0, s>>>(f);
+  if (!f.whole) {
+    const int64_t rows = std::min<int64_t>(std::min(f.a.max_q, f.a.T) * f.group, f.tile_rows);
+    join_kernel<X><<<dim3(W, (unsigned)std::max<int64_t>(rows, 1)), kThreads, 0, s>>>(f);
+  }
 }
 
 }  // namespace
 
+static size_t cuts_bytes(size_t W) { return align_up(W * kWaves * 16, 256); }
+static size_t joined_bytes(size_t W) { return align_up(W * 4, 256); }
 size_t attend_few_workspace(const KvAttend& a, int64_t few) {
   const int tile = few_tile(a, few);
+  if (few_whole(a, tile)) return 0;
   const size_t W = (size_t)few_workgroups(a, tile);
-  return align_up(W * 16, 256) + align_up(2 * W * tile * (a.c.dim + 2) * sizeof(float), 256);
+  return cuts_bytes(W) + joined_bytes(W) + align_up(2 * W * kWaves * tile * (a.c.dim + 2) * sizeof(float), 256);
 }
 
 hipError_t attend_few(const KvAttend& a, int64_t few, void* ws, hipStream_t s) {
@@ -634,11 +876,13 @@ hipError_t attend_few(const KvAttend& a, int64_t few, void* ws, hipStream_t s) {
   f.few = few;
   f.group = a.heads / a.c.heads;
   f.tile_rows = few_tile(a, few);
+  f.whole = few_whole(a, f.tile_rows);
   const size_t es = elem_size(a.dtype);
   f.q_wide = reinterpret_cast<uintptr_t>(a.Q) % 16 == 0 && (size_t)a.q_stride * es % 16 == 0;
   const int W = few_workgroups(a, f.tile_rows);
-  f.heads = reinterpret_cast<int*>(ws);
-  f.parts = reinterpret_cast<float*>(static_cast<char*>(ws) + align_up((size_t)W * 16, 256));
+  f.cuts = reinterpret_cast<int*>(ws);
+  f.joined = reinterpret_cast<int*>(static_cast<char*>(ws) + cuts_bytes(W));
+  f.parts = reinterpret_cast<float*>(static_cast<char*>(ws) + cuts_bytes(W) + joined_bytes(W));
   if (a.dtype == GSI_BF16) launch_few<BF16>(f, W, s);
   else launch_few<F32>(f, W, s);
   return hipGetLastError();
