@@ -41,20 +41,45 @@ __device__ __forceinline__ Span span_of(const KvAttend& a, int b) {
 }
 
 __device__ __forceinline__ float scale_value(int byte) { return __uint_as_float((uint32_t)byte << 23); }
-// 16 elements of a query row from element d on; zero past the head's end or for no row
+// 16 elements of a query row from element d on, as they are stored; zero for no row
 template <class X>
-__device__ __forceinline__ void load_q16(const typename X::storage* row, int d, bool ok, bool wide, float (&x)[16]) {
+struct Query16 {
+  static constexpr int kVectors = sizeof(typename X::storage);
+  u32x4 w[kVectors];
+  __device__ __forceinline__ void load(const typename X::storage* row, int d, bool ok, bool wide) {
 #pragma unroll
-  for (int i = 0; i < 16; ++i) x[i] = 0.f;
-  if (!ok) return;
-  if (wide) {
+    for (int i = 0; i < kVectors; ++i) w[i] = u32x4{0, 0, 0, 0};
+    if (!ok) return;
+    if (wide) {
 #pragma unroll
-    for (int i = 0; i < 16; i += X::kVec) X::load_vec(row + d + i, reinterpret_cast<float(&)[X::kVec]>(x[i]));
-  } else {
+      for (int i = 0; i < kVectors; ++i) w[i] = *reinterpret_cast<const u32x4*>(row + d + 16 / kVectors * i);
+    } else {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = X::load(row, d + i);
+      for (int i = 0; i < 16; ++i) {
+        if constexpr (kVectors == 4) w[i / 4][i % 4] = __float_as_uint(row[d + i]);
+        else w[i / 8][i / 2 % 4] |= (uint32_t)row[d + i] << (16 * (i & 1));
+      }
+    }
   }
-}
+  // term t of CH: eight elements as an operand
+  template <int CH>
+  __device__ __forceinline__ void terms(int eight, bf16x8 (&out)[CH]) const {
+    if constexpr (kVectors == 2) {
+      out[0] = __builtin_bit_cast(bf16x8, w[eight]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float e = __uint_as_float(w[2 * eight + i / 4][i % 4]);
+#pragma unroll
+        for (int t = 0; t < CH; ++t) {
+          const __bf16 v = (__bf16)e;
+          out[t][i] = v;
+          e -= (float)v;
+        }
+      }
+    }
+  }
+};
 
 __device__ __forceinline__ float row16_max(float v) {  // over aligned groups of 16 lanes
   v = fmaxf(v, dpp_move<0xB1>(v));
@@ -67,6 +92,18 @@ __device__ __forceinline__ float row16_sum(float v) {
   v += dpp_move<0x4E>(v);
   v += dpp_move<0x141>(v);
   return v + dpp_move<0x140>(v);
+}
+
+// Rows of tokens that belong to no request: zero.
+template <class X>
+__device__ __forceinline__ void clear_idle_rows(const KvAttend& a) {
+  const int64_t t0 = !a.q_start ? a.T : a.B > 0 ? min(max(a.q_start[a.B], 0), (int)a.T) : 0;
+  typename X::storage* const O = reinterpret_cast<typename X::storage*>(a.O);
+  const int64_t row = (int64_t)a.heads * a.c.dim, all = (int64_t)gridDim.x * gridDim.y * blockDim.x;
+  const int64_t me = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * blockDim.x + threadIdx.x;
+  for (int64_t i = t0 * row + me; i < a.T * row; i += all) X::store(O, i, 0.f);
+  if (a.lse)
+    for (int64_t i = t0 * a.heads + me; i < a.T * a.heads; i += all) a.lse[i] = -INFINITY;
 }
 
 __device__ __forceinline__ void order_lds() { asm volatile("" ::: "memory"); }  // a wave's LDS accesses run in program order

@@ -25,9 +25,9 @@ struct Few {
   int tile_rows;  // rows of a tile
   int q_wide;     // 16-byte loads of queries
   int whole;      // a workgroup takes whole tiles, its waves parts of their keys; else every wave an equal share of all steps
-  float* parts;   // [2 * waves][tile_rows][dim + 2]: sums, maximum, sum of weights of a cut tile
+  float* parts;   // [2 * waves][tile_rows][dim]: sums of a cut tile
+  float2* stats;  // [2 * waves][tile_rows]: their maxima and sums of weights; a maximum of NaN: no part (another wave's place has it)
   int* cuts;      // [waves][4]: the tile that a wave begins and does not end, and the wave that ends it
-  int* joined;    // [workgroups]: whether its waves' parts are in the first one's place
 };
 
 // Tiles of a request and the steps of each (one where there are rows but no keys).  A tile counts as kTileCost units and one for every step: its
@@ -239,29 +239,25 @@ __global__ __launch_bounds__(kThreads, DPL == 16 || NR > 1 ? 2 : 3) void few_ker
   const int D = EXACT ? 16 * DPL : a.c.dim;
   const Ln L(D);
 
-  // tokens of no request
-  {
-    const int64_t t0 = !a.q_start ? a.T : a.B > 0 ? min(max(a.q_start[a.B], 0), (int)a.T) : 0;
-    typename X::storage* const O = reinterpret_cast<typename X::storage*>(a.O);
-    const int64_t row = (int64_t)a.heads * D, me = (int64_t)blockIdx.x * kThreads + threadIdx.x, all = (int64_t)gridDim.x * kThreads;
-    for (int64_t i = t0 * row + me; i < a.T * row; i += all) X::store(O, i, 0.f);
-    if (a.lse)
-      for (int64_t i = t0 * a.heads + me; i < a.T * a.heads; i += all) a.lse[i] = -INFINITY;
-  }
-
   // this wave's units
   const int64_t me = (int64_t)blockIdx.x * kWaves + wave;
   if (!f.whole && threadIdx.x < kWaves) f.cuts[4 * (blockIdx.x * kWaves + threadIdx.x)] = -1;
   int64_t total = scan_requests(f, 0, prefix);
   for (int64_t b0 = kThreads; b0 < a.B; b0 += kThreads) total += scan_requests(f, b0, prefix);
-  if (total == 0) return;
+  if (total == 0) {
+    clear_idle_rows<X>(a);
+    return;
+  }
   const Shares sh = shares_of(total, gridDim.x);
   int64_t u, u_end;
   if (f.whole) {
     u = blockIdx.x;
     u_end = total;
   } else {
-    if (blockIdx.x >= sh.groups) return;
+    if (blockIdx.x >= sh.groups) {
+      clear_idle_rows<X>(a);
+      return;
+    }
     u = sh.first_unit(me);
     u_end = sh.first_unit(me + 1);
   }
@@ -300,7 +296,6 @@ __global__ __launch_bounds__(kThreads, DPL == 16 || NR > 1 ? 2 : 3) void few_ker
     __syncthreads();
     together = stats[0][0][0] != 0.f;
     __syncthreads();
-    if (threadIdx.x == 0) f.joined[blockIdx.x] = together;
   }
 
   const float zscale = a.scale * kLog2e;
@@ -357,6 +352,19 @@ __global__ __launch_bounds__(kThreads, DPL == 16 || NR > 1 ? 2 : 3) void few_ker
     const int64_t code0 = a.c.code_at(0, kvh), scale0 = a.c.scale_at(0, kvh);
     const Where at{a.table + (int64_t)b * a.width, a.c.K + code0, a.c.Ks + scale0, a.c.V + code0, a.c.Vs + scale0,
                    (uint32_t)a.c.code_at(1, 0), (uint32_t)a.c.scale_at(1, 0)};
+    // query rows are requested first: they are converted while keys and values are on their way
+    Query16<X> raw[KW / 2];
+    {
+      const int r = R::row(L.c), rid = tile * TR + r;
+      const bool real = r >= 0 && r < rows;
+      const int tok = real ? rid / f.group : 0, head = kvh * f.group + (real ? rid % f.group : 0);
+      const typename X::storage* const Q = reinterpret_cast<const typename X::storage*>(a.Q) + (int64_t)(sp.t0 + tok) * a.q_stride + (int64_t)head * D;
+#pragma unroll
+      for (int x = 0; x < KW / 2; ++x) {
+        const int d = 8 * KW * L.g + 16 * x;
+        raw[x].load(Q, d, real && d < D, f.q_wide);
+      }
+    }
     const int key_end = min(sp.len, last * kStep);
     int key = first * kStep;
     Keys<DPL> K;
@@ -371,32 +379,16 @@ __global__ __launch_bounds__(kThreads, DPL == 16 || NR > 1 ? 2 : 3) void few_ker
       load_values<DPL>(V, a, at, pv, L, key, D / 2);
     }
 
-    bf16x8 q[CH][KW];
-    {
-      const int r = R::row(L.c), rid = tile * TR + r;
-      const bool real = r >= 0 && r < rows;
-      const int tok = real ? rid / f.group : 0, head = kvh * f.group + (real ? rid % f.group : 0);
-      const typename X::storage* const Q = reinterpret_cast<const typename X::storage*>(a.Q) + (int64_t)(sp.t0 + tok) * a.q_stride + (int64_t)head * D;
+    bf16x8 q[KW][CH];
 #pragma unroll
-      for (int x = 0; x < KW / 2; ++x) {
-        float e[16];
-        const int d = 8 * KW * L.g + 16 * x;
-        load_q16<X>(Q, d, real && d < D, f.q_wide, e);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          if constexpr (R::kFold) {
-            const float h = (float)(__bf16)e[i], m = (float)(__bf16)(e[i] - h);
-            const int t = R::term(L.c);
-            q[0][2 * x + i / 8][i % 8] = (__bf16)(t == 0 ? e[i] : t == 1 ? e[i] - h : e[i] - h - m);
-          } else {
-#pragma unroll
-            for (int t = 0; t < CH; ++t) {
-              const __bf16 v = (__bf16)e[i];
-              q[t][2 * x + i / 8][i % 8] = v;
-              if (t + 1 < CH) e[i] -= (float)v;
-            }
-          }
-        }
+    for (int x = 0; x < KW; ++x) {
+      if constexpr (R::kFold) {
+        bf16x8 all[3];
+        raw[x / 2].template terms<3>(x % 2, all);
+        const int t = R::term(L.c);
+        q[x][0] = t == 0 ? all[0] : t == 1 ? all[1] : all[2];
+      } else {
+        raw[x / 2].template terms<CH>(x % 2, q[x]);
       }
     }
     // the last key that a row sees: by the layout of the scores, and of the output (the same but where terms are folded)
@@ -449,7 +441,7 @@ __global__ __launch_bounds__(kThreads, DPL == 16 || NR > 1 ? 2 : 3) void few_ker
           const float sc = L.kin[x] ? scale_value((K.scale[x] >> (8 * j)) & 255u) : 1.f;
           const bf16x8 k = eight_values(K.w[j][w], sc);
 #pragma unroll
-          for (int t = 0; t < CH; ++t) s[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[t][w], k, s[j], 0, 0, 0);
+          for (int t = 0; t < CH; ++t) s[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[w][t], k, s[j], 0, 0, 0);
         }
       }
       const bool k_there = is_page(a, pk), v_there = is_page(a, pv);
@@ -662,13 +654,14 @@ __global__ __launch_bounds__(kThreads, DPL == 16 || NR > 1 ? 2 : 3) void few_ker
       __syncthreads();
       if (wave == 0) add(1);
     }
+    if (together && !f.whole && wave != 0 && lane < TR) f.stats[2 * me * TR + lane] = make_float2(NAN, 0.f);
     if (!together || wave == 0) {
       const int64_t to = together && !f.whole ? sh.of_group(blockIdx.x + 1) : u_end;  // where this part ends
       const bool complete = f.whole || (first == 0 && to >= seg_begin + per);
       float* part = nullptr;
       if (!complete) {
         // place 2 i: a tile that an earlier wave began; place 2 i + 1: one that begins here and ends elsewhere
-        part = f.parts + (2 * me + (first == 0)) * TR * (D + 2);
+        part = f.parts + (2 * me + (first == 0)) * TR * D;
         if (first == 0 && lane == 0) {
           int* const cut = f.cuts + 4 * me;
           cut[1] = tile;
@@ -698,19 +691,17 @@ __global__ __launch_bounds__(kThreads, DPL == 16 || NR > 1 ? 2 : 3) void few_ker
             }
           if (a.lse && L.c == 0) a.lse[orow] = l[i] == 0.f ? -INFINITY : (m[i] == -INFINITY ? l[i] : (m[i] + log2f(l[i])) * kLn2);
         } else {
-          float* const row = part + r * (D + 2);
           if (DPL * L.c < D)
 #pragma unroll
-            for (int j = 0; j < DPL; j += 2) *reinterpret_cast<f32x2*>(row + DPL * L.c + j) = f32x2{out[i][j], out[i][j + 1]};
-          if (L.c == 0) {
-            row[D] = m[i];
-            row[D + 1] = l[i];
-          }
+            for (int j = 0; j < DPL; j += 4)
+              *reinterpret_cast<f32x4*>(part + r * D + DPL * L.c + j) = f32x4{out[i][j], out[i][j + 1], out[i][j + 2], out[i][j + 3]};
+          if (L.c == 0) f.stats[(2 * me + (first == 0)) * TR + r] = make_float2(m[i], l[i]);
         }
       }
     }
     u = f.whole ? u + gridDim.x : min(u_end, seg_begin + per);
   }
+  clear_idle_rows<X>(a);
 }
 
 // Joins the parts of the tiles that a cut went through, in their order: a workgroup for the cuts that begin in one of few_kernel's and a row, a wave for
@@ -719,7 +710,7 @@ __global__ __launch_bounds__(kThreads, DPL == 16 || NR > 1 ? 2 : 3) void few_ker
 constexpr int kListed = 512;
 template <class X>
 __global__ __launch_bounds__(kThreads) void join_kernel(Few f) {
-  __shared__ float weight[kWaves][kListed];
+  __shared__ float weight[kWaves][kListed], total[kWaves][kListed];
   __shared__ int place[kWaves][kListed];
   __shared__ float lds[kThreads][5];
   const KvAttend& a = f.a;
@@ -743,7 +734,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Few f) {
     // where wave i's part lies (none where its workgroup's first wave has it for the four)
     const auto slot = [&](int i) { return i == w ? 2 * i + 1 : 2 * i; };
     for (int r = blockIdx.y; r < rows; r += gridDim.y) {
-      const auto part = [&](int s) { return f.parts + ((int64_t)s * f.tile_rows + r) * (D + 2); };
+      const auto row_of = [&](int s) { return (int64_t)s * f.tile_rows + r; };
       float top = -INFINITY, sum = 0.f;
       f32x4 o = {0.f, 0.f, 0.f, 0.f};
       // kListed parts at a time; a wave works out the list by itself, the same one in each where four work together
@@ -752,16 +743,18 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Few f) {
         float mine = -INFINITY;
         int n = 0;
         for (int i = i0 + lane; i - lane < i1; i += kWave) {
-          const bool has = i < i1 && (i % kWaves == 0 || !f.joined[i / kWaves]);
-          const float m = has ? part(slot(i))[D] : -INFINITY;
+          const float2 ml = f.stats[row_of(slot(min(i, end)))];
+          const float m = ml.x;
+          const bool has = i < i1 && m == m;
           const uint64_t ballot = __ballot(has);
           if (has) {
             const int at = n + __popcll(ballot & ((1ull << lane) - 1));
             place[wave][at] = slot(i);
             weight[wave][at] = m;
+            total[wave][at] = ml.y;
           }
           n += __popcll(ballot);
-          mine = fmaxf(mine, m);
+          mine = has ? fmaxf(mine, m) : mine;
         }
 #pragma unroll
         for (int x = kWave / 2; x; x >>= 1) mine = fmaxf(mine, __shfl_xor(mine, x, kWave));
@@ -772,14 +765,11 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Few f) {
         order_lds();
 #pragma unroll 8
         for (int y = way; y < n; y += ways) {
-          const float* const p = part(place[wave][y]);
+          const f32x4 v = *reinterpret_cast<const f32x4*>(f.parts + row_of(place[wave][y]) * D + min(d, D - 4));
           const float mv = weight[wave][y], x = mv == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mv - top);
-          const f32x2 lo = *reinterpret_cast<const f32x2*>(p + min(d, D - 4)), hi = *reinterpret_cast<const f32x2*>(p + min(d, D - 4) + 2);
-          sum += p[D + 1] * x;
-          o[0] += lo[0] * x;
-          o[1] += lo[1] * x;
-          o[2] += hi[0] * x;
-          o[3] += hi[1] * x;
+          sum += total[wave][y] * x;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[e] += v[e] * x;
         }
         order_lds();
       }
@@ -834,7 +824,7 @@ int few_workgroups(const KvAttend& a, int tile_rows) {
   const double tiles = (double)few_tiles(a, tile_rows);
   if (few_whole(a, tile_rows)) return (int)std::max(1.0, std::min(tiles, 4096.0));
   const double units = tiles * (double)ceil_div(a.max_len, kStep) / kWaves;
-  return (int)std::max(1.0, std::min(units, 768.0));
+  return (int)std::max(1.0, std::min(units, 512.0));
 }
 
 template <class X, int NR>
@@ -862,12 +852,12 @@ void launch_few(const Few& f, int W, hipStream_t s) {
 }  // namespace
 
 static size_t cuts_bytes(size_t W) { return align_up(W * kWaves * 16, 256); }
-static size_t joined_bytes(size_t W) { return align_up(W * 4, 256); }
+static size_t stats_bytes(size_t W, int tile) { return align_up(2 * W * kWaves * tile * sizeof(float2), 256); }
 size_t attend_few_workspace(const KvAttend& a, int64_t few) {
   const int tile = few_tile(a, few);
   if (few_whole(a, tile)) return 0;
   const size_t W = (size_t)few_workgroups(a, tile);
-  return cuts_bytes(W) + joined_bytes(W) + align_up(2 * W * kWaves * tile * (a.c.dim + 2) * sizeof(float), 256);
+  return cuts_bytes(W) + stats_bytes(W, tile) + align_up(2 * W * kWaves * tile * a.c.dim * sizeof(float), 256);
 }
 
 hipError_t attend_few(const KvAttend& a, int64_t few, void* ws, hipStream_t s) {
@@ -881,8 +871,8 @@ hipError_t attend_few(const KvAttend& a, int64_t few, void* ws, hipStream_t s) {
   f.q_wide = reinterpret_cast<uintptr_t>(a.Q) % 16 == 0 && (size_t)a.q_stride * es % 16 == 0;
   const int W = few_workgroups(a, f.tile_rows);
   f.cuts = reinterpret_cast<int*>(ws);
-  f.joined = reinterpret_cast<int*>(static_cast<char*>(ws) + cuts_bytes(W));
-  f.parts = reinterpret_cast<float*>(static_cast<char*>(ws) + cuts_bytes(W) + joined_bytes(W));
+  f.stats = reinterpret_cast<float2*>(static_cast<char*>(ws) + cuts_bytes(W));
+  f.parts = reinterpret_cast<float*>(static_cast<char*>(ws) + cuts_bytes(W) + stats_bytes(W, f.tile_rows));
   if (a.dtype == GSI_BF16) launch_few<BF16>(f, W, s);
   else launch_few<F32>(f, W, s);
   return hipGetLastError();

@@ -97,20 +97,11 @@ __global__ __launch_bounds__(kThreads, ND <= 4 ? 2 : 1) void prompt_kernel(Promp
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, c = lane & 31, h = lane >> 5;
   constexpr int D = 32 * ND, half = D / 2;
 
-  if (f.zero) {
-    const int64_t t0 = !a.q_start ? a.T : a.B > 0 ? min(max(a.q_start[a.B], 0), (int)a.T) : 0;
-    typename X::storage* const O = reinterpret_cast<typename X::storage*>(a.O);
-    const int64_t row = (int64_t)a.heads * D, all = (int64_t)gridDim.x * gridDim.y * kThreads;
-    const int64_t me = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kThreads + threadIdx.x;
-    for (int64_t i = t0 * row + me; i < a.T * row; i += all) X::store(O, i, 0.f);
-    if (a.lse)
-      for (int64_t i = t0 * a.heads + me; i < a.T * a.heads; i += all) a.lse[i] = -INFINITY;
-  }
-
   // heads of keys run fastest: with eight of them and more, an XCD's cache holds the same ones throughout
   const int kvh = blockIdx.x % a.c.heads;
   int64_t before;
   const int b = __builtin_amdgcn_readfirstlane(owner_of(f, blockIdx.x / a.c.heads, before, scan));
+  if (f.zero) clear_idle_rows<X>(a);
   if (b < 0) return;
   const Span sp = span_of(a, b);
   // the last tile, which sees the most keys, first
@@ -135,17 +126,11 @@ __global__ __launch_bounds__(kThreads, ND <= 4 ? 2 : 1) void prompt_kernel(Promp
     for (int p = 0; p < NP; ++p)
 #pragma unroll
       for (int y = 0; y < 2; ++y) {
-        float e[16];
+        Query16<X> raw;
         const int d = 32 * (2 * p + h) + 16 * y;
-        load_q16<X>(Q, d, real && d < D, f.q_wide, e);
-#pragma unroll
-        for (int t = 0; t < QT; ++t)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const __bf16 v = (__bf16)e[i];
-            q[p][2 * y + i / 8][t][i % 8] = v;
-            if (t + 1 < QT) e[i] -= (float)v;
-          }
+        raw.load(Q, d, real && d < D, f.q_wide);
+        raw.template terms<QT>(0, q[p][2 * y]);
+        raw.template terms<QT>(1, q[p][2 * y + 1]);
       }
   }
 
