@@ -27,6 +27,10 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // 2^kSlack, which costs fp32 sums and bf16 weights nothing, and almost no step rescales what is summed so far.
 constexpr float kSlack = 8.f;
 
+// A score's factor in the exponential, above 0: the largest score is then the largest product, whose factor enters one fused operation with the
+// maximum's subtraction.  A negative scale turns the queries' sign; one of 0 becomes a number that changes no score.
+__device__ __forceinline__ float exponent_scale(float scale) { return fmaxf(fabsf(scale) * kLog2e, 1.17549435e-38f); }
+
 struct Span {  // a request's tokens of the call and its keys
   int t0, n, len;
 };
@@ -41,12 +45,12 @@ __device__ __forceinline__ Span span_of(const KvAttend& a, int b) {
 }
 
 __device__ __forceinline__ float scale_value(int byte) { return __uint_as_float((uint32_t)byte << 23); }
-// 16 elements of a query row from element d on, as they are stored; zero for no row
+// 16 elements of a query row from element d on, as they are stored (minus: with the other sign); zero for no row
 template <class X>
 struct Query16 {
   static constexpr int kVectors = sizeof(typename X::storage);
   u32x4 w[kVectors];
-  __device__ __forceinline__ void load(const typename X::storage* row, int d, bool ok, bool wide) {
+  __device__ __forceinline__ void load(const typename X::storage* row, int d, bool ok, bool wide, bool minus) {
 #pragma unroll
     for (int i = 0; i < kVectors; ++i) w[i] = u32x4{0, 0, 0, 0};
     if (!ok) return;
@@ -59,6 +63,10 @@ struct Query16 {
         if constexpr (kVectors == 4) w[i / 4][i % 4] = __float_as_uint(row[d + i]);
         else w[i / 8][i / 2 % 4] |= (uint32_t)row[d + i] << (16 * (i & 1));
       }
+    }
+    if (minus) {
+#pragma unroll
+      for (int i = 0; i < kVectors; ++i) w[i] ^= kVectors == 4 ? 0x80000000u : 0x80008000u;
     }
   }
   // term t of CH: eight elements as an operand
@@ -105,6 +113,10 @@ __device__ __forceinline__ void clear_idle_rows(const KvAttend& a) {
   if (a.lse)
     for (int64_t i = t0 * a.heads + me; i < a.T * a.heads; i += all) a.lse[i] = -INFINITY;
 }
+
+// A rare path that is to stay a branch: the compiler would compute both sides for every element.  The condition is the same in every lane.
+__device__ __forceinline__ bool rarely(bool x) { return __builtin_expect(__builtin_amdgcn_readfirstlane((int)x), 0); }
+__device__ __forceinline__ void keep_branch() { asm volatile(""); }
 
 __device__ __forceinline__ void order_lds() { asm volatile("" ::: "memory"); }  // a wave's LDS accesses run in program order
 

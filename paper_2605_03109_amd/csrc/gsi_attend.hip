@@ -298,7 +298,7 @@ __global__ __launch_bounds__(kThreads, DPL == 16 || NR > 1 ? 2 : 3) void few_ker
     __syncthreads();
   }
 
-  const float zscale = a.scale * kLog2e;
+  const float zscale = exponent_scale(a.scale);
   // row of the output product: the weights' image and row that lane c's row has, and whether it is the one of the odd elements
   int p_row[NO];
   bool p_odd;
@@ -362,7 +362,7 @@ __global__ __launch_bounds__(kThreads, DPL == 16 || NR > 1 ? 2 : 3) void few_ker
 #pragma unroll
       for (int x = 0; x < KW / 2; ++x) {
         const int d = 8 * KW * L.g + 16 * x;
-        raw[x].load(Q, d, real && d < D, f.q_wide);
+        raw[x].load(Q, d, real && d < D, f.q_wide, a.scale < 0.f);
       }
     }
     const int key_end = min(sp.len, last * kStep);
@@ -454,8 +454,9 @@ __global__ __launch_bounds__(kThreads, DPL == 16 || NR > 1 ? 2 : 3) void few_ker
 #pragma unroll
       for (int i = 0; i < NS; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) z[i][j] = (R::kFold ? s[j][0] + s[j][1] + s[j][2] : s[j][i]) * zscale;
-      if (key + kStep - 1 > lim_low || __any(!k_there || !v_there)) {
+        for (int j = 0; j < 4; ++j) z[i][j] = R::kFold ? s[j][0] + s[j][1] + s[j][2] : s[j][i];
+      if (rarely(key + kStep - 1 > lim_low || __any(!k_there || !v_there))) {
+        keep_branch();
         // the end of the keys, keys that only some rows see, or pages that are not there
         int bad = 0x7fffffff;
 #pragma unroll
@@ -492,13 +493,13 @@ __global__ __launch_bounds__(kThreads, DPL == 16 || NR > 1 ? 2 : 3) void few_ker
 #pragma unroll
       for (int i = 0; i < NS; ++i) {
         top[i] = fmaxf(fmaxf(z[i][0], z[i][1]), fmaxf(z[i][2], z[i][3]));
-        moves |= top[i] > m[i] + kSlack;
+        moves |= top[i] * zscale > m[i] + kSlack;
       }
       if (__any(moves)) {
         float keep[NS];
 #pragma unroll
         for (int i = 0; i < NS; ++i) {
-          const float next = fmaxf(m[i], row16_max(top[i]));
+          const float next = fmaxf(m[i], row16_max(top[i]) * zscale);
           keep[i] = next == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[i] - next);
           m[i] = next;
           l[i] *= keep[i];
@@ -512,7 +513,7 @@ __global__ __launch_bounds__(kThreads, DPL == 16 || NR > 1 ? 2 : 3) void few_ker
         float p[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          p[j] = __builtin_amdgcn_exp2f(z[i][j] - base);
+          p[j] = __builtin_amdgcn_exp2f(fmaf(z[i][j], zscale, -base));
           l[i] += p[j];
         }
 #pragma unroll

@@ -128,7 +128,7 @@ __global__ __launch_bounds__(kThreads, ND <= 4 ? 2 : 1) void prompt_kernel(Promp
       for (int y = 0; y < 2; ++y) {
         Query16<X> raw;
         const int d = 32 * (2 * p + h) + 16 * y;
-        raw.load(Q, d, real && d < D, f.q_wide);
+        raw.load(Q, d, real && d < D, f.q_wide, a.scale < 0.f);
         raw.template terms<QT>(0, q[p][2 * y]);
         raw.template terms<QT>(1, q[p][2 * y + 1]);
       }
@@ -140,7 +140,7 @@ __global__ __launch_bounds__(kThreads, ND <= 4 ? 2 : 1) void prompt_kernel(Promp
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
   float m = -INFINITY, l = 0.f;
-  const float zscale = a.scale * kLog2e;
+  const float zscale = exponent_scale(a.scale);
 
   const int steps = high < 0 ? 0 : high / kStep + 1;
   const int step0 = (int)((int64_t)steps * blockIdx.y / f.splits), step1 = (int)((int64_t)steps * (blockIdx.y + 1) / f.splits);
@@ -161,43 +161,51 @@ __global__ __launch_bounds__(kThreads, ND <= 4 ? 2 : 1) void prompt_kernel(Promp
   const auto entries = [&](int step) {
     Entries r;
 #pragma unroll
-    for (int g = 0; g < 4; ++g) r.e[g] = trow[min((step * kStep + 16 * g) >> a.c.page_shift, last)];
+    for (int g = 0; g < 4; ++g) r.e[g] = __builtin_amdgcn_readfirstlane(trow[min((step * kStep + 16 * g) >> a.c.page_shift, last)]);
     return r;
   };
+  const int uwave = __builtin_amdgcn_readfirstlane(wave);
+  const int64_t code0 = a.c.code_at(0, kvh), scale0 = a.c.scale_at(0, kvh);
+  const uint32_t code_stride = (uint32_t)a.c.code_at(1, 0), scale_stride = (uint32_t)a.c.scale_at(1, 0);
+  struct Four {
+    uint64_t a, b, c, d;
+  };
+  const auto pick = [](Four x, int g) {
+    const uint64_t a = x.a, b = x.b, c = x.c, d = x.d;
+    const uint64_t low = (g & 1) ? b : a, high = (g & 1) ? d : c;
+    return (g & 2) ? high : low;
+  };
+  // word u of the values: 64 ND words to 16 tokens, so that a wave's lie on one page; token u / (4 ND), word u % (4 ND) of it
   const auto bring = [&](int step, const Entries& en) {
     Bring r;
     r.there = 0;
-    int64_t code[4], scale[4];
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
+    const auto place = [&](int g, uint64_t base, uint32_t stride, int each) {
       const bool ok = (uint32_t)en.e[g] < (uint32_t)a.c.n_pages;
       r.there |= ok ? 1 << g : 0;
-      const int64_t page = ok ? en.e[g] : 0;
-      const int off = (step * kStep + 16 * g) & mask;
-      code[g] = a.c.code_at(page, kvh) + (int64_t)off * half;
-      scale[g] = a.c.scale_at(page, kvh) + off;
-    }
-    const auto pick = [](const int64_t (&x)[4], int g) { return g == 0 ? x[0] : g == 1 ? x[1] : g == 2 ? x[2] : x[3]; };
+      return base + (uint64_t)(ok ? (uint32_t)en.e[g] : 0u) * stride + ((step * kStep + 16 * g) & mask) * each;
+    };
+    const Four code{place(0, code0, code_stride, half), place(1, code0, code_stride, half), place(2, code0, code_stride, half), place(3, code0, code_stride, half)};
+    const Four scale{place(0, scale0, scale_stride, 1), place(1, scale0, scale_stride, 1), place(2, scale0, scale_stride, 1), place(3, scale0, scale_stride, 1)};
 #pragma unroll
     for (int i = 0; i < KU; ++i) {
       const int u = i * kThreads + threadIdx.x, t = u % kStep, blk = u / kStep;
-      if (ND % 4 == 0 || blk < ND) r.k[i] = *reinterpret_cast<const u32x4*>(a.c.K + pick(code, t / 16) + (t % 16) * half + blk * 16);
+      if (ND % 4 == 0 || blk < ND) r.k[i] = *reinterpret_cast<const u32x4*>(a.c.K + pick(code, t / 16) + ((t % 16) * half + blk * 16));
     }
     if ((int)threadIdx.x < ND * 16) {
       const int t = threadIdx.x % 16 * 4, blk = threadIdx.x / 16;
-      r.ks = *reinterpret_cast<const uint32_t*>(a.c.Ks + pick(scale, t / 16) + ((int64_t)blk << a.c.page_shift) + t % 16);
+      r.ks = *reinterpret_cast<const uint32_t*>(a.c.Ks + pick(scale, t / 16) + ((blk << a.c.page_shift) + t % 16));
     }
 #pragma unroll
     for (int i = 0; i < ND; ++i) {
-      const int u = i * kThreads + threadIdx.x, t = u / (4 * ND), w = u % (4 * ND);
-      r.v[i] = *reinterpret_cast<const uint32_t*>(a.c.V + pick(code, t / 16) + (t % 16) * half + w * 4);
-      r.vs[i] = a.c.Vs[pick(scale, t / 16) + ((int64_t)(w / 4) << a.c.page_shift) + t % 16];
+      const int g = (i * kWaves + uwave) / ND, u = i * kThreads + threadIdx.x, t = u / (4 * ND), w = u % (4 * ND);
+      r.v[i] = *reinterpret_cast<const uint32_t*>(a.c.V + pick(code, g) + (uint32_t)((t % 16) * half + w * 4));
+      r.vs[i] = (a.c.Vs + pick(scale, g))[(uint32_t)(((w / 4) << a.c.page_shift) + t % 16)];
     }
     return r;
   };
   const auto stage = [&](int step, const Bring& r) {
     char* const at = lds + (step & 1) * M::kSize;
-    const bool special = step * kStep + kStep - 1 > low || r.there != 15;
+    const bool special = rarely(step * kStep + kStep - 1 > low || r.there != 15);
 #pragma unroll
     for (int i = 0; i < KU; ++i) {
       const int u = i * kThreads + threadIdx.x;
@@ -209,6 +217,7 @@ __global__ __launch_bounds__(kThreads, ND <= 4 ? 2 : 1) void prompt_kernel(Promp
       const int u = i * kThreads + threadIdx.x, t = u / (4 * ND), w = u % (4 * ND);
       uint32_t word = r.v[i], vs = r.vs[i];
       if (special) {
+        keep_branch();
         // 0 times what is not seen, or seen by some rows only, has to be 0: NaN goes to its rows by `spoiled`
         const bool seen = step * kStep + t < sp.len && (r.there >> (t / 16) & 1);
         if (seen && vs == 255u) atomicMin(&spoiled[step % 3][w / 4], step * kStep + t);
@@ -270,11 +279,8 @@ __global__ __launch_bounds__(kThreads, ND <= 4 ? 2 : 1) void prompt_kernel(Promp
             for (int t = 0; t < QT; ++t) s[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[p][w][t], s[y], 0, 0, 0);
           }
       }
-#pragma unroll
-      for (int y = 0; y < 2; ++y)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[y][i] *= zscale;
-      if (key + kStep - 1 > wave_low || there != 15) {
+      if (rarely(key + kStep - 1 > wave_low || there != 15)) {
+        keep_branch();
 #pragma unroll
         for (int y = 0; y < 2; ++y)
 #pragma unroll
@@ -283,7 +289,8 @@ __global__ __launch_bounds__(kThreads, ND <= 4 ? 2 : 1) void prompt_kernel(Promp
             s[y][i] = key + t <= lim && (there >> (2 * y + i / 8) & 1) ? s[y][i] : -INFINITY;
           }
       }
-      if (key + kStep - 1 > low || there != 15) {  // as stage() has it
+      if (rarely(key + kStep - 1 > low || there != 15)) {  // as stage() has it
+        keep_branch();
 #pragma unroll
         for (int d = 0; d < ND; ++d)
           if (spoiled[step % 3][d] <= lim) {
@@ -296,9 +303,9 @@ __global__ __launch_bounds__(kThreads, ND <= 4 ? 2 : 1) void prompt_kernel(Promp
       for (int y = 0; y < 2; ++y)
 #pragma unroll
         for (int i = 0; i < 16; ++i) top = fmaxf(top, s[y][i]);
-      if (__any(top > m + kSlack)) {
+      if (__any(top * zscale > m + kSlack)) {
         top = fmaxf(top, __shfl_xor(top, 32, kWave));
-        const float next_m = fmaxf(m, top);
+        const float next_m = fmaxf(m, top * zscale);
         const float keep = next_m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - next_m);
         m = next_m;
         l *= keep;
@@ -312,7 +319,7 @@ __global__ __launch_bounds__(kThreads, ND <= 4 ? 2 : 1) void prompt_kernel(Promp
       for (int y = 0; y < 2; ++y)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          s[y][i] = __builtin_amdgcn_exp2f(s[y][i] - base);
+          s[y][i] = __builtin_amdgcn_exp2f(fmaf(s[y][i], zscale, -base));
           l += s[y][i];
         }
 #pragma unroll
