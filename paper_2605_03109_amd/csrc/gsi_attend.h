@@ -118,6 +118,9 @@ __device__ __forceinline__ void clear_idle_rows(const KvAttend& a) {
 __device__ __forceinline__ bool rarely(bool x) { return __builtin_expect(__builtin_amdgcn_readfirstlane((int)x), 0); }
 __device__ __forceinline__ void keep_branch() { asm volatile(""); }
 
+// Ends the wait for an operand that was loaded before a loop: the compiler would wait for all loads there, in every step.
+__device__ __forceinline__ void arrive(bf16x8& x) { asm volatile("" : "+v"(x)); }
+
 __device__ __forceinline__ void order_lds() { asm volatile("" ::: "memory"); }  // a wave's LDS accesses run in program order
 
 }  // namespace

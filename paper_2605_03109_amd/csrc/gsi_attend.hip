@@ -390,6 +390,8 @@ __global__ __launch_bounds__(kThreads, DPL == 16 || NR > 1 ? 2 : 3) void few_ker
       } else {
         raw[x / 2].template terms<CH>(x % 2, q[x]);
       }
+#pragma unroll
+      for (int t = 0; t < CH; ++t) arrive(q[x][t]);
     }
     // the last key that a row sees: by the layout of the scores, and of the output (the same but where terms are folded)
     int lim[NS], lim_o[NS];

@@ -161,7 +161,7 @@ __global__ __launch_bounds__(kThreads, ND <= 4 ? 2 : 1) void prompt_kernel(Promp
   const auto entries = [&](int step) {
     Entries r;
 #pragma unroll
-    for (int g = 0; g < 4; ++g) r.e[g] = __builtin_amdgcn_readfirstlane(trow[min((step * kStep + 16 * g) >> a.c.page_shift, last)]);
+    for (int g = 0; g < 4; ++g) r.e[g] = trow[min((step * kStep + 16 * g) >> a.c.page_shift, last)];
     return r;
   };
   const int uwave = __builtin_amdgcn_readfirstlane(wave);
@@ -175,21 +175,36 @@ __global__ __launch_bounds__(kThreads, ND <= 4 ? 2 : 1) void prompt_kernel(Promp
     const uint64_t low = (g & 1) ? b : a, high = (g & 1) ? d : c;
     return (g & 2) ? high : low;
   };
+  // the same in every lane of a wave
+  const auto uniform = [](uint64_t x) {
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)x);
+  };
+  // token and block of the i-th block of keys: where the blocks of 16 tokens fill waves, a wave's lie on one page
+  struct TokenBlock {
+    int t, blk;
+  };
+  const auto key_block = [](int i) {
+    const int u = i * kThreads + threadIdx.x;
+    if constexpr (ND % 4 == 0) return TokenBlock{u / (16 * ND) * 16 + u % 16, u % (16 * ND) / 16};
+    else return TokenBlock{u % kStep, u / kStep};
+  };
   // word u of the values: 64 ND words to 16 tokens, so that a wave's lie on one page; token u / (4 ND), word u % (4 ND) of it
   const auto bring = [&](int step, const Entries& en) {
     Bring r;
     r.there = 0;
     const auto place = [&](int g, uint64_t base, uint32_t stride, int each) {
-      const bool ok = (uint32_t)en.e[g] < (uint32_t)a.c.n_pages;
+      const uint32_t page = __builtin_amdgcn_readfirstlane(en.e[g]);  // (here, a step later: its load is not waited for where it is requested)
+      const bool ok = page < (uint32_t)a.c.n_pages;
       r.there |= ok ? 1 << g : 0;
-      return base + (uint64_t)(ok ? (uint32_t)en.e[g] : 0u) * stride + ((step * kStep + 16 * g) & mask) * each;
+      return base + (uint64_t)(ok ? page : 0u) * stride + ((step * kStep + 16 * g) & mask) * each;
     };
     const Four code{place(0, code0, code_stride, half), place(1, code0, code_stride, half), place(2, code0, code_stride, half), place(3, code0, code_stride, half)};
     const Four scale{place(0, scale0, scale_stride, 1), place(1, scale0, scale_stride, 1), place(2, scale0, scale_stride, 1), place(3, scale0, scale_stride, 1)};
 #pragma unroll
     for (int i = 0; i < KU; ++i) {
-      const int u = i * kThreads + threadIdx.x, t = u % kStep, blk = u / kStep;
-      if (ND % 4 == 0 || blk < ND) r.k[i] = *reinterpret_cast<const u32x4*>(a.c.K + pick(code, t / 16) + ((t % 16) * half + blk * 16));
+      const auto [t, blk] = key_block(i);
+      if constexpr (ND % 4 == 0) r.k[i] = *reinterpret_cast<const u32x4*>(a.c.K + uniform(pick(code, (i * kWaves + uwave) / (ND / 4))) + (uint32_t)((t % 16) * half + blk * 16));
+      else if (blk < ND) r.k[i] = *reinterpret_cast<const u32x4*>(a.c.K + pick(code, t / 16) + ((t % 16) * half + blk * 16));
     }
     if ((int)threadIdx.x < ND * 16) {
       const int t = threadIdx.x % 16 * 4, blk = threadIdx.x / 16;
@@ -197,9 +212,9 @@ __global__ __launch_bounds__(kThreads, ND <= 4 ? 2 : 1) void prompt_kernel(Promp
     }
 #pragma unroll
     for (int i = 0; i < ND; ++i) {
-      const int g = (i * kWaves + uwave) / ND, u = i * kThreads + threadIdx.x, t = u / (4 * ND), w = u % (4 * ND);
-      r.v[i] = *reinterpret_cast<const uint32_t*>(a.c.V + pick(code, g) + (uint32_t)((t % 16) * half + w * 4));
-      r.vs[i] = (a.c.Vs + pick(scale, g))[(uint32_t)(((w / 4) << a.c.page_shift) + t % 16)];
+      const int g = ND % 4 == 0 ? i / (ND / 4) : (i * kWaves + uwave) / ND, u = i * kThreads + threadIdx.x, t = u / (4 * ND), w = u % (4 * ND);
+      r.v[i] = *reinterpret_cast<const uint32_t*>(a.c.V + uniform(pick(code, g)) + (uint32_t)((t % 16) * half + w * 4));
+      r.vs[i] = (a.c.Vs + uniform(pick(scale, g)))[(uint32_t)(((w / 4) << a.c.page_shift) + t % 16)];
     }
     return r;
   };
@@ -208,8 +223,8 @@ __global__ __launch_bounds__(kThreads, ND <= 4 ? 2 : 1) void prompt_kernel(Promp
     const bool special = rarely(step * kStep + kStep - 1 > low || r.there != 15);
 #pragma unroll
     for (int i = 0; i < KU; ++i) {
-      const int u = i * kThreads + threadIdx.x;
-      if (ND % 4 == 0 || u / kStep < ND) *reinterpret_cast<u32x4*>(at + M::kKeys + u * 16) = r.k[i];
+      const auto [t, blk] = key_block(i);
+      if (ND % 4 == 0 || blk < ND) *reinterpret_cast<u32x4*>(at + M::kKeys + (blk * kStep + t) * 16) = r.k[i];
     }
     if ((int)threadIdx.x < ND * 16) *reinterpret_cast<uint32_t*>(at + M::kScales + threadIdx.x * 4) = r.ks;
 #pragma unroll
@@ -240,6 +255,12 @@ __global__ __launch_bounds__(kThreads, ND <= 4 ? 2 : 1) void prompt_kernel(Promp
     there = r.there;
     stage(step0, r);
   }
+#pragma unroll
+  for (int p = 0; p < NP; ++p)
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+#pragma unroll
+      for (int t = 0; t < QT; ++t) arrive(q[p][w][t]);
   __syncthreads();
   const int vlane = (4 * h + ((lane & 15) >> 2)) * M::kStride + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
   for (int step = step0; step < step1; ++step) {
