@@ -9,7 +9,7 @@ namespace gsi {
 // that share it) and those of more.
 hipError_t attend_few(const KvAttend& a, int64_t few, void* ws, hipStream_t s);
 size_t attend_few_workspace(const KvAttend& a, int64_t few);
-hipError_t attend_prompt(const KvAttend& a, int64_t few, bool zero, void* ws, hipStream_t s);  // zero: it writes the tokens of no request
+hipError_t attend_prompt(const KvAttend& a, int64_t few, bool zero, void* ws, hipStream_t s);  // zero: it clears the rows of no request
 size_t attend_prompt_workspace(const KvAttend& a);
 
 namespace {
@@ -45,6 +45,101 @@ __device__ __forceinline__ Span span_of(const KvAttend& a, int b) {
 }
 
 __device__ __forceinline__ float scale_value(int byte) { return __uint_as_float((uint32_t)byte << 23); }
+__device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {  // both at least 0; the quotient of 64 bits takes a hundred instructions
+  return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
+// Work in units, by request: `units` says how many a span has.  The spans of 256 requests at a time and prefix sums of their units lie in LDS; all
+// threads of a workgroup of 256 call these functions together.
+constexpr int kScan = 256;
+struct Prefix {
+  int64_t incl[kScan];
+  int64_t sums[kScan / kWave];
+  Span span[kScan];
+};
+template <class U>
+__device__ __forceinline__ int64_t scan_requests(const KvAttend& a, int64_t b0, Prefix& x, U units) {
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int64_t b = b0 + threadIdx.x;
+  int64_t v = 0;
+  Span sp{0, 0, 0};
+  if (b < a.B) {
+    sp = span_of(a, (int)b);
+    v = units(sp);
+  }
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) {
+    const int64_t up = __shfl_up(v, o, kWave);
+    if (lane >= o) v += up;
+  }
+  __syncthreads();
+  if (lane == kWave - 1) x.sums[wave] = v;
+  __syncthreads();
+  int64_t total = 0;
+#pragma unroll
+  for (int w = 0; w < kScan / kWave; ++w) {
+    if (w < wave) v += x.sums[w];
+    total += x.sums[w];
+  }
+  x.incl[threadIdx.x] = v;
+  x.span[threadIdx.x] = sp;
+  __syncthreads();
+  return total;
+}
+template <class U>
+__device__ __forceinline__ int64_t total_units(const KvAttend& a, Prefix& x, U units) {
+  int64_t total = scan_requests(a, 0, x, units);
+  for (int64_t b0 = kScan; b0 < a.B; b0 += kScan) total += scan_requests(a, b0, x, units);
+  return total;
+}
+// (the first 256 requests' spans stay in LDS unless there are more requests)
+__device__ __forceinline__ Span span_at(const KvAttend& a, const Prefix& x, int b) { return a.B <= kScan ? x.span[b] : span_of(a, b); }
+
+// The request of unit u (a wave's own) after total_units, and the units before it; the first one where u is past the end.
+struct Place {
+  int b;
+  int64_t before;
+};
+template <class U>
+__device__ __forceinline__ Place place_of(const KvAttend& a, Prefix& x, int64_t total, int64_t u, U units) {
+  Place p{0, 0};
+  int64_t carry = 0;
+  bool found = false;
+  for (int64_t b0 = 0; b0 < a.B && carry < total; b0 += kScan) {
+    const int64_t here = a.B <= kScan ? total : scan_requests(a, b0, x, units);
+    if (!found && u < carry + here) {
+      int lo = 0, hi = kScan - 1;  // the first request whose inclusive sum is above u - carry
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (x.incl[mid] > u - carry) hi = mid;
+        else lo = mid + 1;
+      }
+      p.b = (int)b0 + lo;
+      p.before = carry + (lo ? x.incl[lo - 1] : 0);
+      found = true;
+    }
+    carry += here;
+  }
+  p.b = __builtin_amdgcn_readfirstlane(p.b);
+  return p;
+}
+
+// Equal shares of the units for the workgroups, `least` units at least each.
+struct Shares {
+  int64_t total, groups, each, more;  // each: units of a workgroup; the first `more` have one more
+  __device__ __forceinline__ int64_t of_group(int64_t g) const { return each * g + min(g, more); }
+  __device__ __forceinline__ int64_t units_of_group(int64_t g) const { return each + (g < more ? 1 : 0); }
+  __device__ __forceinline__ int64_t group_of(int64_t u) const {
+    const int64_t big = more * (each + 1);
+    return u < big ? divide(u, each + 1) : more + divide(u - big, each);
+  }
+};
+__device__ __forceinline__ Shares shares_of(int64_t total, int64_t groups, int64_t least) {
+  groups = max((int64_t)1, min(groups, divide(total, least)));
+  const int64_t each = divide(total, groups);
+  return Shares{total, groups, each, total - each * groups};
+}
+
 // 16 elements of a query row from element d on, as they are stored (minus: with the other sign); zero for no row
 template <class X>
 struct Query16 {

@@ -42,70 +42,17 @@ __device__ __forceinline__ Steps steps_of(const Few& f, const Span& s) {
 }
 __device__ __forceinline__ int tile_units(const Few& f, const Steps& st) { return f.whole ? 1 : st.per_tile + kTileCost; }
 
-__device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {  // both at least 0; the quotient of 64 bits takes a hundred instructions
-  return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+// Wave i of the launch takes the units [first_unit(i), first_unit(i + 1)): a quarter of its workgroup's.  No wave before the last that has any is
+// without one.
+__device__ __forceinline__ int64_t first_unit(const Shares& s, int64_t i) {
+  const int64_t g = i / kWaves, k = i % kWaves;
+  if (s.total < kWaves) return min(i, s.total);
+  return s.of_group(g) + s.units_of_group(g) * k / kWaves;
 }
-
-// The spans of 256 requests at a time, and prefix sums of their units, in LDS.
-struct Prefix {
-  int64_t incl[kThreads];
-  int64_t sums[kWaves];
-  Span span[kThreads];
-};
-__device__ __forceinline__ int64_t scan_requests(const Few& f, int64_t b0, Prefix& x) {
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const int64_t b = b0 + threadIdx.x;
-  int64_t v = 0;
-  Span sp{0, 0, 0};
-  if (b < f.a.B) {
-    sp = span_of(f.a, (int)b);
-    const Steps st = steps_of(f, sp);
-    v = (int64_t)st.tiles * f.a.c.heads * tile_units(f, st);
-  }
-#pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) {
-    const int64_t up = __shfl_up(v, o, kWave);
-    if (lane >= o) v += up;
-  }
-  __syncthreads();
-  if (lane == kWave - 1) x.sums[wave] = v;
-  __syncthreads();
-  int64_t total = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    if (w < wave) v += x.sums[w];
-    total += x.sums[w];
-  }
-  x.incl[threadIdx.x] = v;
-  x.span[threadIdx.x] = sp;
-  __syncthreads();
-  return total;
-}
-// (the first 256 requests' spans stay in LDS unless there are more requests)
-__device__ __forceinline__ Span span_at(const Few& f, const Prefix& x, int b) { return f.a.B <= kThreads ? x.span[b] : span_of(f.a, b); }
-
-// Wave i of the launch takes the units [first_unit(i), first_unit(i + 1)): equal shares for the workgroups, four units at least, and
-// for their waves.  No wave before the last that has any is without one.
-struct Shares {
-  int64_t total, groups, each, more;  // each: units of a workgroup; the first `more` have one more
-  __device__ __forceinline__ int64_t of_group(int64_t g) const { return each * g + min(g, more); }
-  __device__ __forceinline__ int64_t first_unit(int64_t i) const {
-    const int64_t g = i / kWaves, k = i % kWaves;
-    if (total < kWaves) return min(i, total);
-    return of_group(g) + (each + (g < more ? 1 : 0)) * k / kWaves;
-  }
-  __device__ __forceinline__ int64_t owner(int64_t u) const {  // the wave that has unit u
-    const int64_t big = more * (each + 1);
-    const int64_t g = total < kWaves ? 0 : u < big ? divide(u, each + 1) : more + divide(u - big, each);
-    int64_t i = g * kWaves + kWaves - 1;
-    while (first_unit(i) > u) --i;
-    return i;
-  }
-};
-__device__ __forceinline__ Shares shares_of(int64_t total, int64_t groups) {
-  groups = max((int64_t)1, min(groups, total / kWaves));
-  const int64_t each = divide(total, groups);
-  return Shares{total, groups, each, total - each * groups};
+__device__ __forceinline__ int64_t owner(const Shares& s, int64_t u) {  // the wave that has unit u
+  int64_t i = (s.total < kWaves ? 0 : s.group_of(u)) * kWaves + kWaves - 1;
+  while (first_unit(s, i) > u) --i;
+  return i;
 }
 
 // ---- operands -------------------------------------------------------------------------------------------------
@@ -242,13 +189,16 @@ __global__ __launch_bounds__(kThreads, DPL == 16 || NR > 1 ? 2 : 3) void few_ker
   // this wave's units
   const int64_t me = (int64_t)blockIdx.x * kWaves + wave;
   if (!f.whole && threadIdx.x < kWaves) f.cuts[4 * (blockIdx.x * kWaves + threadIdx.x)] = -1;
-  int64_t total = scan_requests(f, 0, prefix);
-  for (int64_t b0 = kThreads; b0 < a.B; b0 += kThreads) total += scan_requests(f, b0, prefix);
+  const auto units = [&](const Span& sp) {
+    const Steps st = steps_of(f, sp);
+    return (int64_t)st.tiles * a.c.heads * tile_units(f, st);
+  };
+  const int64_t total = total_units(a, prefix, units);
   if (total == 0) {
     clear_idle_rows<X>(a);
     return;
   }
-  const Shares sh = shares_of(total, gridDim.x);
+  const Shares sh = shares_of(total, gridDim.x, kWaves);
   int64_t u, u_end;
   if (f.whole) {
     u = blockIdx.x;
@@ -258,37 +208,17 @@ __global__ __launch_bounds__(kThreads, DPL == 16 || NR > 1 ? 2 : 3) void few_ker
       clear_idle_rows<X>(a);
       return;
     }
-    u = sh.first_unit(me);
-    u_end = sh.first_unit(me + 1);
+    u = first_unit(sh, me);
+    u_end = first_unit(sh, me + 1);
   }
-  int b = 0;
-  int64_t before = 0;
-  {
-    // the request of unit u
-    int64_t carry = 0;
-    bool found = false;
-    for (int64_t b0 = 0; b0 < a.B && carry < total; b0 += kThreads) {
-      const int64_t here = a.B <= kThreads ? total : scan_requests(f, b0, prefix);
-      if (!found && u < carry + here) {
-        int lo = 0, hi = kThreads - 1;  // the first request whose inclusive sum is above u - carry
-        while (lo < hi) {
-          const int mid = (lo + hi) >> 1;
-          if (prefix.incl[mid] > u - carry) hi = mid;
-          else lo = mid + 1;
-        }
-        b = (int)b0 + lo;
-        before = carry + (lo ? prefix.incl[lo - 1] : 0);
-        found = true;
-      }
-      carry += here;
-    }
-    b = __builtin_amdgcn_readfirstlane(b);
-  }
+  const Place place = place_of(a, prefix, total, u, units);
+  int b = place.b;
+  int64_t before = place.before;
   // whether the workgroup's units are all steps of one tile: its waves' parts are then joined here
   bool together = f.whole;
   if (!f.whole) {
     if (threadIdx.x == 0) {
-      const Steps st = steps_of(f, span_at(f, prefix, b));
+      const Steps st = steps_of(f, span_at(a, prefix, b));
       const int64_t per = tile_units(f, st), g0 = sh.of_group(blockIdx.x) - before, g1 = sh.of_group(blockIdx.x + 1) - before;
       const int64_t tile = divide(g0, per);
       stats[0][0][0] = total >= kWaves && g0 >= tile * per + (g0 > tile * per ? kTileCost : 0) && g1 <= (tile + 1) * per && g1 - g0 >= kWaves * (kTileCost + 1) ? 1.f : 0.f;
@@ -315,14 +245,14 @@ __global__ __launch_bounds__(kThreads, DPL == 16 || NR > 1 ? 2 : 3) void few_ker
   constexpr int kImage = TR * kPStride;
 
   while (u < u_end) {
-    Span sp = span_at(f, prefix, b);
+    Span sp = span_at(a, prefix, b);
     Steps st = steps_of(f, sp);
     int per = tile_units(f, st);
     int64_t mine = (int64_t)st.tiles * a.c.heads * per;
     while (u >= before + mine) {  // the next request with rows
       before += mine;
       ++b;
-      sp = span_at(f, prefix, b);
+      sp = span_at(a, prefix, b);
       st = steps_of(f, sp);
       per = tile_units(f, st);
       mine = (int64_t)st.tiles * a.c.heads * per;
@@ -669,7 +599,7 @@ __global__ __launch_bounds__(kThreads, DPL == 16 || NR > 1 ? 2 : 3) void few_ker
           int* const cut = f.cuts + 4 * me;
           cut[1] = tile;
           cut[2] = kvh;
-          cut[3] = (int)sh.owner(seg_begin + per - 1);
+          cut[3] = (int)owner(sh, seg_begin + per - 1);
           cut[0] = b;
         }
       }

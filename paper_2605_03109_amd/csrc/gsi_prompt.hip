@@ -25,9 +25,12 @@ struct Prompt {
   int64_t few;   // requests of at most so many rows are another kernel's
   int group;
   int q_wide;
-  int splits;    // parts of a tile's keys
-  int zero;      // whether this launch writes the tokens of no request
-  float* parts;  // [splits][T * heads][dim + 2]: sums, maximum, sum of weights
+  int zero;       // whether this launch clears the rows of tokens of no request
+  int fold;       // whole tiles: of a request, the one half from the last on, then the other from the first on
+  // shares (null: a workgroup takes a whole tile)
+  f32x4* parts;   // [2 * workgroups][dim / 8][256]: a thread's sums of a cut tile
+  float2* stats;  // [2 * workgroups][128]: a row's maximum and sum of weights; a maximum of NaN: no part
+  int* cuts;      // [workgroups][4]: the tile that a workgroup begins and does not end, and the one that ends it
 };
 
 template <int ND>
@@ -41,37 +44,30 @@ __device__ __forceinline__ int64_t tiles_of(const Prompt& f, const Span& s) {
   return rows > f.few ? (rows + kTile - 1) / kTile : 0;
 }
 
-// the request of tile `slot` and the tiles before it; -1: there are not so many
-__device__ __forceinline__ int owner_of(const Prompt& f, int64_t slot, int64_t& before, int64_t* lds) {
-  const int lane = threadIdx.x % kWave;
-  if (threadIdx.x == 0) lds[4] = -1;
-  int64_t carry = 0;
-  for (int64_t b0 = 0; b0 < f.a.B; b0 += kThreads) {
-    const int64_t b = b0 + threadIdx.x;
-    const int64_t mine = b < f.a.B ? tiles_of(f, span_of(f.a, (int)b)) : 0;
-    int64_t incl = mine;
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-      const int64_t up = __shfl_up(incl, o, kWave);
-      if (lane >= o) incl += up;
-    }
-    __syncthreads();
-    if (lane == kWave - 1) lds[threadIdx.x / kWave] = incl;
-    __syncthreads();
-    int64_t at = carry;
-    for (int w = 0; w < (int)threadIdx.x / kWave; ++w) at += lds[w];
-    at += incl - mine;
-    if (slot >= at && slot < at + mine) {
-      lds[4] = b;
-      lds[5] = at;
-    }
-    carry += lds[0] + lds[1] + lds[2] + lds[3];
-    if (slot < carry) break;
-  }
-  __syncthreads();
-  before = lds[5];
-  return (int)lds[4];
+__device__ __forceinline__ int high_of(const Prompt& f, const Span& s, int tile) {  // the last key that a row of the tile sees
+  return s.len - s.n + (int)((uint32_t)min(tile * kTile + kTile - 1, s.n * f.group - 1) / (uint32_t)f.group);
 }
+__device__ __forceinline__ int steps_of(const Prompt& f, const Span& s, int tile) { return max(0, high_of(f, s, tile)) / kStep + 1; }
+
+// What a tile costs, in keys times the heads of a group: the keys that its rows see, which grow by 128 from tile to tile, and two steps for its
+// queries and its output.  A closed form: the cost of a request's first t tiles is 64 t^2 + (a - 64) t.
+struct Cost {
+  int64_t a;  // of the first tile
+  int64_t tiles;
+  __device__ __forceinline__ Cost(const Prompt& f, const Span& s)
+      : a((int64_t)f.group * (max(0, s.len - s.n) + 2 * kStep) + kTile), tiles(tiles_of(f, s)) {}
+  __device__ __forceinline__ int64_t of_tile(int64_t t) const { return a + kTile * t; }
+  __device__ __forceinline__ int64_t before(int64_t t) const { return (kTile / 2 * t + a - kTile / 2) * t; }
+  __device__ __forceinline__ int64_t all() const { return before(tiles); }
+  __device__ __forceinline__ int64_t tile_at(int64_t u) const {  // the tile with before(t) <= u < before(t + 1)
+    const double half = 0.5 * (double)(a - kTile / 2);
+    int64_t t = (int64_t)((sqrt(half * half + kTile / 2 * (double)u) - half) / (kTile / 2));
+    t = min(max(t, (int64_t)0), tiles - 1);
+    while (t > 0 && before(t) > u) --t;
+    while (t + 1 < tiles && before(t + 1) <= u) ++t;
+    return t;
+  }
+};
 
 __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
   const bf16x2 v = {(__bf16)a, (__bf16)b};
@@ -85,27 +81,111 @@ __device__ __forceinline__ u32x4 eight_values(uint32_t w, float scale) {
   return u32x4{two_values<0>(w, scale), two_values<1>(w, scale), two_values<2>(w, scale), two_values<3>(w, scale)};
 }
 
+// A lane's elements of a row of the output: 32 d + 8 i + 4 h .. of its ND blocks from block d0 on.
+template <class X, int ND>
+__device__ __forceinline__ void store_rows(const KvAttend& a, const f32x16 (&o)[ND], float m, float l, int64_t orow, int h, int d0 = 0) {
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  typename X::storage* const out = reinterpret_cast<typename X::storage*>(a.O) + orow * a.c.dim + 32 * d0 + 4 * h;
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      typename X::storage* const p = out + 32 * d + 8 * i;
+      const float x[4] = {o[d][4 * i] * inv, o[d][4 * i + 1] * inv, o[d][4 * i + 2] * inv, o[d][4 * i + 3] * inv};
+      if constexpr (sizeof(*p) == 4) *reinterpret_cast<f32x4*>(p) = f32x4{x[0], x[1], x[2], x[3]};
+      else *reinterpret_cast<u32x2*>(p) = u32x2{bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3])};
+    }
+  if (a.lse && h == 0 && d0 == 0) a.lse[orow] = l == 0.f ? -INFINITY : (m == -INFINITY ? l : (m + log2f(l)) * kLn2);
+}
+
 template <class X, int ND>
 __global__ __launch_bounds__(kThreads, ND <= 4 ? 2 : 1) void prompt_kernel(Prompt f) {
   constexpr bool F = sizeof(typename X::storage) == 4;
   constexpr int QT = F ? 3 : 1, PT = F ? 3 : 1, NP = (ND + 1) / 2, KU = (ND + 3) / 4;
   using M = Lds<ND>;
   extern __shared__ __align__(16) char lds[];
-  __shared__ int64_t scan[6];
+  __shared__ Prefix prefix;
   __shared__ int spoiled[3][ND];  // first token of a step whose value is NaN, by block: three steps' worth, one of them being cleared
   const KvAttend& a = f.a;
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, c = lane & 31, h = lane >> 5;
   constexpr int D = 32 * ND, half = D / 2;
 
-  // heads of keys run fastest: with eight of them and more, an XCD's cache holds the same ones throughout
-  const int kvh = blockIdx.x % a.c.heads;
-  int64_t before;
-  const int b = __builtin_amdgcn_readfirstlane(owner_of(f, blockIdx.x / a.c.heads, before, scan));
-  if (f.zero) clear_idle_rows<X>(a);
-  if (b < 0) return;
-  const Span sp = span_of(a, b);
-  // the last tile, which sees the most keys, first
-  const int tile = (int)(tiles_of(f, sp) - 1 - (blockIdx.x / a.c.heads - before));
+  int kvh, b, tile;
+  int64_t u = 0, u_end = 1, before = 0;  // shares: this workgroup's units, and those before request b
+  // workgroups run round the eight caches of the chip: those of consecutive shares are taken to one
+  const int64_t me = !f.parts ? blockIdx.x : gridDim.x % 8 == 0 ? blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8 : blockIdx.x;
+  Shares sh{};
+  if (!f.parts) {
+    // heads of keys run fastest: with eight of them and more, a cache holds the same ones throughout
+    const auto units = [&](const Span& s) { return tiles_of(f, s); };
+    const int64_t total = total_units(a, prefix, units), slot = blockIdx.x / a.c.heads;
+    const Place p = place_of(a, prefix, total, slot, units);
+    if (f.zero) clear_idle_rows<X>(a);
+    if (slot >= total) return;
+    b = p.b;
+    kvh = blockIdx.x % a.c.heads;
+    const int64_t n = tiles_of(f, span_at(a, prefix, b)), i = slot - p.before;
+    // The last tiles see the most keys and come first.  Where all workgroups are resident at once, a unit has the i-th and the i-th of the second
+    // half: that half runs the other way, and what two workgroups of a unit do together is about the same everywhere.
+    tile = (int)(!f.fold || i < (n + 1) / 2 ? n - 1 - i : i - (n + 1) / 2);
+  } else {
+    const auto units = [&](const Span& s) { return a.c.heads * Cost(f, s).all(); };
+    const int64_t total = total_units(a, prefix, units);
+    sh = shares_of(total, gridDim.x, 8 * kStep * f.group);
+    u = sh.of_group(me);
+    u_end = total == 0 || me >= sh.groups ? u : sh.of_group(me + 1);
+    const Place p = place_of(a, prefix, total, u, units);
+    b = p.b;
+    before = p.before;
+    if (f.zero) clear_idle_rows<X>(a);
+    if (threadIdx.x == 0) f.cuts[4 * me] = -1;
+  }
+  const int uwave = __builtin_amdgcn_readfirstlane(wave);
+  const float zscale = exponent_scale(a.scale);
+  const int last = (int)a.width - 1, mask = a.c.page() - 1;
+  const uint32_t code_stride = (uint32_t)a.c.code_at(1, 0), scale_stride = (uint32_t)a.c.scale_at(1, 0);
+
+  while (u < u_end) {
+  Span sp = span_at(a, prefix, b);
+  int step0 = 0, step1;
+  int64_t stop = u_end;
+  if (!f.parts) {
+    step1 = steps_of(f, sp, tile);
+  } else {
+    Cost cost(f, sp);
+    while (u >= before + a.c.heads * cost.all()) {  // the next request with tiles
+      before += a.c.heads * cost.all();
+      ++b;
+      sp = span_at(a, prefix, b);
+      cost = Cost(f, sp);
+    }
+    const int64_t all = cost.all();
+    kvh = (int)divide(u - before, all);
+    const int64_t at = u - before - kvh * all, t = cost.tile_at(at), own = cost.of_tile(t), off = at - cost.before(t);
+    tile = (int)t;
+    const int64_t end = u - off + own;
+    stop = min(u_end, end);
+    const int steps = steps_of(f, sp, tile);
+    // a boundary lies in front of the step that has its share of the tile's cost: the same for the workgroups on both its sides
+    const auto step_at = [&](int64_t x) { return (int)((double)steps * (double)x / (double)own); };
+    step0 = step_at(off);
+    step1 = stop == end ? steps : step_at(stop - (u - off));
+  }
+  b = __builtin_amdgcn_readfirstlane(b);
+  tile = __builtin_amdgcn_readfirstlane(tile);
+  kvh = __builtin_amdgcn_readfirstlane(kvh);
+  step0 = __builtin_amdgcn_readfirstlane(step0);
+  step1 = __builtin_amdgcn_readfirstlane(step1);
+  sp.t0 = __builtin_amdgcn_readfirstlane(sp.t0);
+  sp.n = __builtin_amdgcn_readfirstlane(sp.n);
+  sp.len = __builtin_amdgcn_readfirstlane(sp.len);
+  const bool ends = !f.parts || step1 == steps_of(f, sp, tile), complete = step0 == 0 && ends;
+  if (step0 >= step1) {
+    // the boundaries on both sides lie in front of one step: no part of the tile
+    if (step0 > 0 && threadIdx.x < kTile) f.stats[2 * me * kTile + threadIdx.x] = make_float2(NAN, 0.f);
+    u = stop;
+    continue;
+  }
   const int all_rows = sp.n * f.group, row0 = tile * kTile, shift0 = sp.len - sp.n;
 
   const int rid = row0 + 32 * wave + c;
@@ -116,7 +196,7 @@ __global__ __launch_bounds__(kThreads, ND <= 4 ? 2 : 1) void prompt_kernel(Promp
   const int wave_first = row0 + 32 * wave, wave_last = min(wave_first + 31, all_rows - 1);
   const int wave_high = wave_first < all_rows ? shift0 + wave_last / f.group : -1;
   const int wave_low = wave_first < all_rows ? shift0 + wave_first / f.group : -1;
-  const int high = shift0 + min(row0 + kTile - 1, all_rows - 1) / f.group, low = shift0 + row0 / f.group;
+  const int low = shift0 + row0 / f.group;
 
   // query rows: the operand's elements 8 h + u of product (p, w) are elements 32 (2 p + h) + 8 w + u
   bf16x8 q[NP][4][QT];
@@ -140,12 +220,7 @@ __global__ __launch_bounds__(kThreads, ND <= 4 ? 2 : 1) void prompt_kernel(Promp
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
   float m = -INFINITY, l = 0.f;
-  const float zscale = exponent_scale(a.scale);
-
-  const int steps = high < 0 ? 0 : high / kStep + 1;
-  const int step0 = (int)((int64_t)steps * blockIdx.y / f.splits), step1 = (int)((int64_t)steps * (blockIdx.y + 1) / f.splits);
   const int32_t* const trow = a.table + (int64_t)b * a.width;
-  const int last = (int)a.width - 1, mask = a.c.page() - 1;
 
   // what a thread brings of a step: blocks of keys (one token's 32 codes), scale bytes of four keys, words of values (8 codes) with their scale
   struct Bring {
@@ -164,9 +239,7 @@ __global__ __launch_bounds__(kThreads, ND <= 4 ? 2 : 1) void prompt_kernel(Promp
     for (int g = 0; g < 4; ++g) r.e[g] = trow[min((step * kStep + 16 * g) >> a.c.page_shift, last)];
     return r;
   };
-  const int uwave = __builtin_amdgcn_readfirstlane(wave);
   const int64_t code0 = a.c.code_at(0, kvh), scale0 = a.c.scale_at(0, kvh);
-  const uint32_t code_stride = (uint32_t)a.c.code_at(1, 0), scale_stride = (uint32_t)a.c.scale_at(1, 0);
   struct Four {
     uint64_t a, b, c, d;
   };
@@ -382,70 +455,79 @@ __global__ __launch_bounds__(kThreads, ND <= 4 ? 2 : 1) void prompt_kernel(Promp
   }
 
   l += __shfl_xor(l, 32, kWave);
-  if (!real) return;
-  const int64_t orow = (int64_t)(sp.t0 + tok) * a.heads + head;
-  if (f.splits == 1) {
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    typename X::storage* const out = reinterpret_cast<typename X::storage*>(a.O) + orow * D;
-#pragma unroll
-    for (int d = 0; d < ND; ++d)
-#pragma unroll
-      for (int i = 0; i < 16; i += 4) {
-        typename X::storage* const p = out + 32 * d + 2 * i + 4 * h;
-        if constexpr (F) *reinterpret_cast<f32x4*>(p) = f32x4{o[d][i] * inv, o[d][i + 1] * inv, o[d][i + 2] * inv, o[d][i + 3] * inv};
-        else *reinterpret_cast<u32x2*>(p) = u32x2{bf16_pair(o[d][i] * inv, o[d][i + 1] * inv), bf16_pair(o[d][i + 2] * inv, o[d][i + 3] * inv)};
-      }
-    if (a.lse && h == 0) a.lse[orow] = l == 0.f ? -INFINITY : (m == -INFINITY ? l : (m + log2f(l)) * kLn2);
+  if (complete) {
+    if (real) store_rows<X, ND>(a, o, m, l, (int64_t)(sp.t0 + tok) * a.heads + head, h);
   } else {
-    float* const out = f.parts + ((int64_t)blockIdx.y * a.T * a.heads + orow) * (D + 2);
+    // place 2 i: a tile that an earlier workgroup began; place 2 i + 1: one that begins here and ends elsewhere
+    const int64_t place = 2 * me + (step0 == 0);
+    f32x4* const part = f.parts + place * (D / 8) * kThreads + threadIdx.x;
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
-      for (int i = 0; i < 16; i += 2) *reinterpret_cast<f32x2*>(out + 32 * d + 8 * (i / 4) + 4 * h + i % 4) = f32x2{o[d][i], o[d][i + 1]};
-    if (h == 0) {
-      out[D] = m;
-      out[D + 1] = l;
+      for (int i = 0; i < 4; ++i) part[(4 * d + i) * kThreads] = f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
+    if (h == 0) f.stats[place * kTile + 32 * wave + c] = make_float2(m, l);
+    if (step0 == 0 && threadIdx.x == 0) {
+      int* const cut = f.cuts + 4 * me;
+      cut[1] = tile;
+      cut[2] = kvh;
+      const Cost cost(f, sp);
+      cut[3] = (int)sh.group_of(before + kvh * cost.all() + cost.before(tile + 1) - 1);
+      cut[0] = b;
     }
+  }
+  u = stop;
   }
 }
 
-// Joins the parts of a tile's keys, a workgroup per token and head, in their order.
+// Joins the parts of a cut tile in their order: a workgroup for each 32 elements of the tile that another has begun and not ended, whose threads
+// have the rows and elements that those of prompt_kernel had.
 template <class X>
-__global__ __launch_bounds__(kKvMaxDim) void join_parts(Prompt f) {
+__global__ __launch_bounds__(kThreads) void join_tiles(Prompt f) {
   const KvAttend& a = f.a;
-  const int t = blockIdx.x, head = blockIdx.y, D = a.c.dim, d = threadIdx.x;
-  int lo = 0, hi = (int)a.B;  // the request with q_start[lo] <= t < q_start[lo + 1]
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if ((a.q_start ? a.q_start[mid] : mid) <= t) lo = mid;
-    else hi = mid;
+  const int w = blockIdx.x, d = blockIdx.y, b = f.cuts[4 * w];
+  if (b < 0) return;
+  const int tile = f.cuts[4 * w + 1], kvh = f.cuts[4 * w + 2], end = f.cuts[4 * w + 3];
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, c = lane & 31, h = lane >> 5;
+  const Span sp = span_of(a, b);
+  const int rid = tile * kTile + 32 * wave + c;
+  const auto place = [&](int i) -> int64_t { return i == w ? 2 * i + 1 : 2 * i; };
+  float top = -INFINITY, sum = 0.f;
+  f32x16 o[1];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) o[0][i] = 0.f;
+  for (int i = w; i <= end; ++i) top = fmaxf(top, f.stats[place(i) * kTile + 32 * wave + c].x);  // (a maximum of NaN is passed over)
+  for (int i = w; i <= end; ++i) {
+    const float2 ml = f.stats[place(i) * kTile + 32 * wave + c];
+    if (ml.x != ml.x) continue;  // the same for all threads
+    const float k = ml.x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml.x - top);
+    sum += ml.y * k;
+    const f32x4* const part = f.parts + (place(i) * (a.c.dim / 8) + 4 * d) * kThreads + threadIdx.x;
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+      const f32x4 v = part[y * kThreads];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[0][4 * y + e] += v[e] * k;
+    }
   }
-  const Span sp = span_of(a, lo);
-  if (t < sp.t0 || t >= sp.t0 + sp.n || tiles_of(f, sp) == 0) return;
-  const int64_t orow = (int64_t)t * a.heads + head;
-  const float* const p0 = f.parts + orow * (D + 2);
-  const int64_t next = a.T * a.heads * (int64_t)(D + 2);
-  float top = -INFINITY;
-  for (int i = 0; i < f.splits; ++i) top = fmaxf(top, p0[i * next + D]);
-  float sum = 0.f, o = 0.f;
-  for (int i = 0; i < f.splits; ++i) {
-    const float* const p = p0 + i * next;
-    const float k = p[D] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(p[D] - top);
-    sum += p[D + 1] * k;
-    if (d < D) o += p[d] * k;
-  }
-  if (d < D) X::store(reinterpret_cast<typename X::storage*>(a.O), orow * D + d, sum == 0.f ? 0.f : o / sum);
-  if (a.lse && d == 0) a.lse[orow] = sum == 0.f ? -INFINITY : (top == -INFINITY ? sum : (top + log2f(sum)) * kLn2);
+  if (rid >= sp.n * f.group) return;
+  const int64_t orow = (int64_t)(sp.t0 + rid / f.group) * a.heads + kvh * f.group + rid % f.group;
+  store_rows<X, 1>(a, o, top, sum, orow, h, d);
 }
 
 int64_t prompt_slots(const KvAttend& a) { return ceil_div(a.T * (a.heads / a.c.heads), kTile) + a.B; }
 
-// Parts of the keys of every tile: where the tiles leave the chip idle (two workgroups a unit), as many as fill it, of 256 keys at least.
-int prompt_splits(const KvAttend& a) {
-  const int64_t rows = a.T * (a.heads / a.c.heads);
-  const int64_t tiles = std::max<int64_t>(1, rows / kTile) * a.c.heads;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(512 / tiles, a.max_len / 256));
+// Workgroups that are resident at once: two a unit, one where a wave has more than half the registers.
+int prompt_resident(const KvAttend& a) { return a.c.dim <= 128 ? 512 : 256; }
+// Whether the keys of all tiles are dealt out in equal shares: where tiles by themselves would leave workgroups idle, or are long enough that the parts of
+// cut tiles cost little beside them (in steps; each workgroup's two parts are written, read and joined).  us a call, shares / whole tiles: six ragged
+// fp32 prompts of 90 to 700 tokens, 24 heads over 8 of 96, 90 / 143; chunks of 512 tokens behind up to 15000 keys 410 / 472; 2048
+// tokens x 32 heads x 128 from the first on, a tile for every workgroup, 81 / 70.
+bool prompt_shares(const KvAttend& a) {
+  const double tiles = (double)a.c.heads * (double)ceil_div(a.T * (a.heads / a.c.heads), kTile), resident = prompt_resident(a);
+  return a.max_len > 16 * kStep && (tiles < 0.75 * resident || tiles * (double)a.max_len / kStep > 48.0 * resident);
 }
+size_t parts_bytes(const KvAttend& a, size_t W) { return 2 * W * kTile * a.c.dim * sizeof(float); }
+size_t stats_bytes(size_t W) { return 2 * W * kTile * sizeof(float2); }
 
 template <class X, int ND>
 hipError_t launch_prompt(const Prompt& f, hipStream_t s) {
@@ -453,8 +535,13 @@ hipError_t launch_prompt(const Prompt& f, hipStream_t s) {
   static LdsLimit limit;
   if (bytes > 60 * 1024)
     if (hipError_t e = limit.allow((const void*)prompt_kernel<X, ND>, bytes); e != hipSuccess) return e;
-  prompt_kernel<X, ND><<<dim3((unsigned)(prompt_slots(f.a) * f.a.c.heads), f.splits), kThreads, bytes, s>>>(f);
-  if (f.splits > 1) join_parts<X><<<dim3((unsigned)f.a.T, f.a.heads), kKvMaxDim, 0, s>>>(f);
+  if (!f.parts) {
+    prompt_kernel<X, ND><<<(unsigned)(prompt_slots(f.a) * f.a.c.heads), kThreads, bytes, s>>>(f);
+  } else {
+    const int W = prompt_resident(f.a);
+    prompt_kernel<X, ND><<<W, kThreads, bytes, s>>>(f);
+    join_tiles<X><<<dim3(W, ND), kThreads, 0, s>>>(f);
+  }
   return hipGetLastError();
 }
 template <class X>
@@ -474,8 +561,9 @@ hipError_t launch_prompt(const Prompt& f, hipStream_t s) {
 }  // namespace
 
 size_t attend_prompt_workspace(const KvAttend& a) {
-  const int n = prompt_splits(a);
-  return n > 1 ? align_up((size_t)n * a.T * a.heads * (a.c.dim + 2) * sizeof(float), 256) : 0;
+  if (!prompt_shares(a)) return 0;
+  const size_t W = prompt_resident(a);
+  return parts_bytes(a, W) + stats_bytes(W) + align_up(W * 16, 256);
 }
 
 hipError_t attend_prompt(const KvAttend& a, int64_t few, bool zero, void* ws, hipStream_t s) {
@@ -485,9 +573,15 @@ hipError_t attend_prompt(const KvAttend& a, int64_t few, bool zero, void* ws, hi
   f.group = a.heads / a.c.heads;
   const size_t es = elem_size(a.dtype);
   f.q_wide = reinterpret_cast<uintptr_t>(a.Q) % 16 == 0 && (size_t)a.q_stride * es % 16 == 0;
-  f.splits = prompt_splits(a);
   f.zero = zero;
-  f.parts = reinterpret_cast<float*>(ws);
+  f.fold = prompt_slots(a) * a.c.heads <= prompt_resident(a) + a.B * a.c.heads;
+  if (prompt_shares(a)) {
+    const size_t W = prompt_resident(a);
+    char* const p = static_cast<char*>(ws);
+    f.parts = reinterpret_cast<f32x4*>(p);
+    f.stats = reinterpret_cast<float2*>(p + parts_bytes(a, W));
+    f.cuts = reinterpret_cast<int*>(p + parts_bytes(a, W) + stats_bytes(W));
+  }
   return a.dtype == GSI_BF16 ? launch_prompt<BF16>(f, s) : launch_prompt<F32>(f, s);
 }
 
