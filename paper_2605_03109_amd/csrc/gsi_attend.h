@@ -140,10 +140,10 @@ __device__ __forceinline__ Shares shares_of(int64_t total, int64_t groups, int64
   return Shares{total, groups, each, total - each * groups};
 }
 
-// 16 elements of a query row from element d on, as they are stored (minus: with the other sign); zero for no row
-template <class X>
-struct Query16 {
-  static constexpr int kVectors = sizeof(typename X::storage);
+// N elements (8 or 16) of a query row from element d on, as they are stored (minus: with the other sign); zero for no row
+template <class X, int N>
+struct QueryPart {
+  static constexpr int kSize = sizeof(typename X::storage), kVectors = N * kSize / 16;
   u32x4 w[kVectors];
   __device__ __forceinline__ void load(const typename X::storage* row, int d, bool ok, bool wide, bool minus) {
 #pragma unroll
@@ -151,23 +151,23 @@ struct Query16 {
     if (!ok) return;
     if (wide) {
 #pragma unroll
-      for (int i = 0; i < kVectors; ++i) w[i] = *reinterpret_cast<const u32x4*>(row + d + 16 / kVectors * i);
+      for (int i = 0; i < kVectors; ++i) w[i] = *reinterpret_cast<const u32x4*>(row + d + 16 / kSize * i);
     } else {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        if constexpr (kVectors == 4) w[i / 4][i % 4] = __float_as_uint(row[d + i]);
+      for (int i = 0; i < N; ++i) {
+        if constexpr (kSize == 4) w[i / 4][i % 4] = __float_as_uint(row[d + i]);
         else w[i / 8][i / 2 % 4] |= (uint32_t)row[d + i] << (16 * (i & 1));
       }
     }
     if (minus) {
 #pragma unroll
-      for (int i = 0; i < kVectors; ++i) w[i] ^= kVectors == 4 ? 0x80000000u : 0x80008000u;
+      for (int i = 0; i < kVectors; ++i) w[i] ^= kSize == 4 ? 0x80000000u : 0x80008000u;
     }
   }
   // term t of CH: eight elements as an operand
   template <int CH>
   __device__ __forceinline__ void terms(int eight, bf16x8 (&out)[CH]) const {
-    if constexpr (kVectors == 2) {
+    if constexpr (kSize == 2) {
       out[0] = __builtin_bit_cast(bf16x8, w[eight]);
     } else {
 #pragma unroll
@@ -212,6 +212,12 @@ __device__ __forceinline__ void clear_idle_rows(const KvAttend& a) {
 // A rare path that is to stay a branch: the compiler would compute both sides for every element.  The condition is the same in every lane.
 __device__ __forceinline__ bool rarely(bool x) { return __builtin_expect(__builtin_amdgcn_readfirstlane((int)x), 0); }
 __device__ __forceinline__ void keep_branch() { asm volatile(""); }
+
+// Reads of LDS stay in front of this point: the compiler would request each right before its use and wait for all of its latency.
+__device__ __forceinline__ void hold_lds() { __builtin_amdgcn_sched_barrier(0x41f); }
+
+// Nothing is moved across this point.
+__device__ __forceinline__ void hold_all() { __builtin_amdgcn_sched_barrier(0); }
 
 // Ends the wait for an operand that was loaded before a loop: the compiler would wait for all loads there, in every step.
 __device__ __forceinline__ void arrive(bf16x8& x) { asm volatile("" : "+v"(x)); }

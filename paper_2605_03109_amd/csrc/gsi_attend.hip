@@ -283,7 +283,7 @@ __global__ __launch_bounds__(kThreads, DPL == 16 || NR > 1 ? 2 : 3) void few_ker
     const Where at{a.table + (int64_t)b * a.width, a.c.K + code0, a.c.Ks + scale0, a.c.V + code0, a.c.Vs + scale0,
                    (uint32_t)a.c.code_at(1, 0), (uint32_t)a.c.scale_at(1, 0)};
     // query rows are requested first: they are converted while keys and values are on their way
-    Query16<X> raw[KW / 2];
+    QueryPart<X, 16> raw[KW / 2];
     {
       const int r = R::row(L.c), rid = tile * TR + r;
       const bool real = r >= 0 && r < rows;

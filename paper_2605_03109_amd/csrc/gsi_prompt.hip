@@ -3,8 +3,8 @@
 // A workgroup of four waves takes 128 rows (tokens times the heads that share a head of keys), 32 a wave, and 64 keys a step.  Scores and
 // outputs are kept transposed, tokens by rows and elements by rows: a row's scores then lie in two lanes, its maximum and its sum
 // need no exchange but one, and the weights are the second product's operand as they come out of the first (the tokens of its
-// contraction taken in the order of the accumulator's registers).  Keys lie in LDS as they are held, 16 bytes a block, and every wave converts
-// what it reads; values are converted once, on their way to LDS, and read there with the transposing reads.
+// contraction taken in the order of the accumulator's registers).  Keys and values are converted once, on their way to LDS; values are read
+// there with the transposing reads.
 #include <algorithm>
 
 #include "gsi_attend.h"
@@ -36,7 +36,8 @@ struct Prompt {
 template <int ND>
 struct Lds {  // of one step
   static constexpr int kStride = 64 * (ND | 1);  // bytes of a token's values: four tokens lie in distinct banks
-  static constexpr int kKeys = 0, kScales = ND * kStep * 16, kValues = kScales + ND * kStep, kSize = kValues + kStep * kStride;
+  // keys: pieces of eight elements, of all tokens one after another; then the values
+  static constexpr int kKeys = 0, kValues = 4 * ND * kStep * 16, kSize = kValues + kStep * kStride;
 };
 
 __device__ __forceinline__ int64_t tiles_of(const Prompt& f, const Span& s) {
@@ -101,8 +102,11 @@ __device__ __forceinline__ void store_rows(const KvAttend& a, const f32x16 (&o)[
 template <class X, int ND>
 __global__ __launch_bounds__(kThreads, ND <= 4 ? 2 : 1) void prompt_kernel(Prompt f) {
   constexpr bool F = sizeof(typename X::storage) == 4;
-  constexpr int QT = F ? 3 : 1, PT = F ? 3 : 1, NP = (ND + 1) / 2, KU = (ND + 3) / 4;
+  constexpr int QT = F ? 3 : 1, PT = F ? 3 : 1, NP = 2 * ND, KU = (ND + 3) / 4;
   using M = Lds<ND>;
+  // One wave a SIMD: nothing else hides what a read of LDS takes.  (ND <= 4: registers for it are dearer, us with / without 419 / 408 on long contexts; heads
+  // of 256, 2048 tokens x 16 heads: 111 / 123)
+  constexpr bool kAhead = ND > 4;
   extern __shared__ __align__(16) char lds[];
   __shared__ Prefix prefix;
   __shared__ int spoiled[3][ND];  // first token of a step whose value is NaN, by block: three steps' worth, one of them being cleared
@@ -198,20 +202,16 @@ __global__ __launch_bounds__(kThreads, ND <= 4 ? 2 : 1) void prompt_kernel(Promp
   const int wave_low = wave_first < all_rows ? shift0 + wave_first / f.group : -1;
   const int low = shift0 + row0 / f.group;
 
-  // query rows: the operand's elements 8 h + u of product (p, w) are elements 32 (2 p + h) + 8 w + u
-  bf16x8 q[NP][4][QT];
+  // query rows: the operand's elements 8 h + u of product p are elements 16 p + 8 h + u
+  bf16x8 q[NP][QT];
   {
     const typename X::storage* const Q = reinterpret_cast<const typename X::storage*>(a.Q) + (int64_t)(sp.t0 + tok) * a.q_stride + (int64_t)head * D;
 #pragma unroll
-    for (int p = 0; p < NP; ++p)
-#pragma unroll
-      for (int y = 0; y < 2; ++y) {
-        Query16<X> raw;
-        const int d = 32 * (2 * p + h) + 16 * y;
-        raw.load(Q, d, real && d < D, f.q_wide, a.scale < 0.f);
-        raw.template terms<QT>(0, q[p][2 * y]);
-        raw.template terms<QT>(1, q[p][2 * y + 1]);
-      }
+    for (int p = 0; p < NP; ++p) {
+      QueryPart<X, 8> raw;
+      raw.load(Q, 16 * p + 8 * h, real, f.q_wide, a.scale < 0.f);
+      raw.template terms<QT>(0, q[p]);
+    }
   }
 
   f32x16 o[ND];
@@ -222,72 +222,36 @@ __global__ __launch_bounds__(kThreads, ND <= 4 ? 2 : 1) void prompt_kernel(Promp
   float m = -INFINITY, l = 0.f;
   const int32_t* const trow = a.table + (int64_t)b * a.width;
 
-  // what a thread brings of a step: blocks of keys (one token's 32 codes), scale bytes of four keys, words of values (8 codes) with their scale
+  // A wave brings 16 tokens of a step, which lie on one page: a thread blocks of keys (one token's 32 codes) and words of values (8 codes), each with its
+  // scale byte.
   struct Bring {
     u32x4 k[KU];
-    uint32_t ks;
+    uint32_t ks[KU];
     uint32_t v[ND];
     uint32_t vs[ND];
     int there;  // a bit for each 16 tokens whose page is there
   };
-  struct Entries {
-    int e[4];
-  };
-  const auto entries = [&](int step) {
-    Entries r;
-#pragma unroll
-    for (int g = 0; g < 4; ++g) r.e[g] = trow[min((step * kStep + 16 * g) >> a.c.page_shift, last)];
-    return r;
-  };
   const int64_t code0 = a.c.code_at(0, kvh), scale0 = a.c.scale_at(0, kvh);
-  struct Four {
-    uint64_t a, b, c, d;
-  };
-  const auto pick = [](Four x, int g) {
-    const uint64_t a = x.a, b = x.b, c = x.c, d = x.d;
-    const uint64_t low = (g & 1) ? b : a, high = (g & 1) ? d : c;
-    return (g & 2) ? high : low;
-  };
-  // the same in every lane of a wave
-  const auto uniform = [](uint64_t x) {
-    return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)x);
-  };
-  // token and block of the i-th block of keys: where the blocks of 16 tokens fill waves, a wave's lie on one page
-  struct TokenBlock {
-    int t, blk;
-  };
-  const auto key_block = [](int i) {
-    const int u = i * kThreads + threadIdx.x;
-    if constexpr (ND % 4 == 0) return TokenBlock{u / (16 * ND) * 16 + u % 16, u % (16 * ND) / 16};
-    else return TokenBlock{u % kStep, u / kStep};
-  };
-  // word u of the values: 64 ND words to 16 tokens, so that a wave's lie on one page; token u / (4 ND), word u % (4 ND) of it
-  const auto bring = [&](int step, const Entries& en) {
+  const auto entry = [&](int step) { return trow[min((step * kStep + 16 * (lane & 3)) >> a.c.page_shift, last)]; };  // lane i: of the step's 16 (i % 4) .. tokens
+  const auto bring = [&](int step, int en) {
     Bring r;
-    r.there = 0;
-    const auto place = [&](int g, uint64_t base, uint32_t stride, int each) {
-      const uint32_t page = __builtin_amdgcn_readfirstlane(en.e[g]);  // (here, a step later: its load is not waited for where it is requested)
-      const bool ok = page < (uint32_t)a.c.n_pages;
-      r.there |= ok ? 1 << g : 0;
-      return base + (uint64_t)(ok ? page : 0u) * stride + ((step * kStep + 16 * g) & mask) * each;
-    };
-    const Four code{place(0, code0, code_stride, half), place(1, code0, code_stride, half), place(2, code0, code_stride, half), place(3, code0, code_stride, half)};
-    const Four scale{place(0, scale0, scale_stride, 1), place(1, scale0, scale_stride, 1), place(2, scale0, scale_stride, 1), place(3, scale0, scale_stride, 1)};
+    r.there = (int)__ballot((uint32_t)en < (uint32_t)a.c.n_pages) & 15;
+    const uint32_t page = r.there >> uwave & 1 ? __builtin_amdgcn_readlane(en, uwave) : 0;  // another page's keys: they are not seen
+    const int off = (step * kStep + 16 * uwave) & mask;
+    const uint64_t code = code0 + (uint64_t)page * code_stride + off * half, scale = scale0 + (uint64_t)page * scale_stride + off;
 #pragma unroll
     for (int i = 0; i < KU; ++i) {
-      const auto [t, blk] = key_block(i);
-      if constexpr (ND % 4 == 0) r.k[i] = *reinterpret_cast<const u32x4*>(a.c.K + uniform(pick(code, (i * kWaves + uwave) / (ND / 4))) + (uint32_t)((t % 16) * half + blk * 16));
-      else if (blk < ND) r.k[i] = *reinterpret_cast<const u32x4*>(a.c.K + pick(code, t / 16) + ((t % 16) * half + blk * 16));
-    }
-    if ((int)threadIdx.x < ND * 16) {
-      const int t = threadIdx.x % 16 * 4, blk = threadIdx.x / 16;
-      r.ks = *reinterpret_cast<const uint32_t*>(a.c.Ks + pick(scale, t / 16) + ((blk << a.c.page_shift) + t % 16));
+      const int u = i * kWave + lane, t = u % 16, blk = u / 16;
+      if (ND % 4 == 0 || blk < ND) {
+        r.k[i] = *reinterpret_cast<const u32x4*>(a.c.K + code + (uint32_t)(t * half + blk * 16));
+        r.ks[i] = (a.c.Ks + scale)[(uint32_t)((blk << a.c.page_shift) + t)];
+      }
     }
 #pragma unroll
     for (int i = 0; i < ND; ++i) {
-      const int g = ND % 4 == 0 ? i / (ND / 4) : (i * kWaves + uwave) / ND, u = i * kThreads + threadIdx.x, t = u / (4 * ND), w = u % (4 * ND);
-      r.v[i] = *reinterpret_cast<const uint32_t*>(a.c.V + uniform(pick(code, g)) + (uint32_t)((t % 16) * half + w * 4));
-      r.vs[i] = (a.c.Vs + uniform(pick(scale, g)))[(uint32_t)(((w / 4) << a.c.page_shift) + t % 16)];
+      const int u = i * kWave + lane, t = u / (4 * ND), w = u % (4 * ND);
+      r.v[i] = *reinterpret_cast<const uint32_t*>(a.c.V + code + (uint32_t)(t * half + w * 4));
+      r.vs[i] = (a.c.Vs + scale)[(uint32_t)(((w / 4) << a.c.page_shift) + t)];
     }
     return r;
   };
@@ -296,18 +260,21 @@ __global__ __launch_bounds__(kThreads, ND <= 4 ? 2 : 1) void prompt_kernel(Promp
     const bool special = rarely(step * kStep + kStep - 1 > low || r.there != 15);
 #pragma unroll
     for (int i = 0; i < KU; ++i) {
-      const auto [t, blk] = key_block(i);
-      if (ND % 4 == 0 || blk < ND) *reinterpret_cast<u32x4*>(at + M::kKeys + (blk * kStep + t) * 16) = r.k[i];
+      const int u = i * kWave + lane, t = 16 * uwave + u % 16, blk = u / 16;
+      if (ND % 4 == 0 || blk < ND) {
+        const float scale = scale_value(r.ks[i]);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) *reinterpret_cast<u32x4*>(at + M::kKeys + ((4 * blk + w) * kStep + t) * 16) = eight_values(r.k[i][w], scale);
+      }
     }
-    if ((int)threadIdx.x < ND * 16) *reinterpret_cast<uint32_t*>(at + M::kScales + threadIdx.x * 4) = r.ks;
 #pragma unroll
     for (int i = 0; i < ND; ++i) {
-      const int u = i * kThreads + threadIdx.x, t = u / (4 * ND), w = u % (4 * ND);
+      const int u = i * kWave + lane, t = 16 * uwave + u / (4 * ND), w = u % (4 * ND);
       uint32_t word = r.v[i], vs = r.vs[i];
       if (special) {
         keep_branch();
         // 0 times what is not seen, or seen by some rows only, has to be 0: NaN goes to its rows by `spoiled`
-        const bool seen = step * kStep + t < sp.len && (r.there >> (t / 16) & 1);
+        const bool seen = step * kStep + t < sp.len && (r.there >> uwave & 1);
         if (seen && vs == 255u) atomicMin(&spoiled[step % 3][w / 4], step * kStep + t);
         if (!seen || vs == 255u) {
           word = 0;
@@ -321,19 +288,17 @@ __global__ __launch_bounds__(kThreads, ND <= 4 ? 2 : 1) void prompt_kernel(Promp
   if ((int)threadIdx.x < 3 * ND) spoiled[threadIdx.x / ND][threadIdx.x % ND] = 0x7fffffff;
   __syncthreads();
   int there = 15;
-  Entries en{};
-  if (step0 < step1) {
-    const Bring r = bring(step0, entries(step0));
-    en = entries(step0 + 1);
+  int en;
+  {
+    const Bring r = bring(step0, entry(step0));
+    en = entry(step0 + 1);
     there = r.there;
     stage(step0, r);
   }
 #pragma unroll
   for (int p = 0; p < NP; ++p)
 #pragma unroll
-    for (int w = 0; w < 4; ++w)
-#pragma unroll
-      for (int t = 0; t < QT; ++t) arrive(q[p][w][t]);
+    for (int t = 0; t < QT; ++t) arrive(q[p][t]);
   __syncthreads();
   const int vlane = (4 * h + ((lane & 15) >> 2)) * M::kStride + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
   for (int step = step0; step < step1; ++step) {
@@ -341,7 +306,7 @@ __global__ __launch_bounds__(kThreads, ND <= 4 ? 2 : 1) void prompt_kernel(Promp
     const bool more = step + 1 < step1;
     if (more) {
       next = bring(step + 1, en);
-      en = entries(step + 2);
+      en = entry(step + 2);  // (taken a step later: it is not waited for here)
     }
     if ((int)threadIdx.x < ND) spoiled[(step + 2) % 3][threadIdx.x] = 0x7fffffff;
     const char* const at = lds + (step & 1) * M::kSize;
@@ -352,26 +317,26 @@ __global__ __launch_bounds__(kThreads, ND <= 4 ? 2 : 1) void prompt_kernel(Promp
       for (int y = 0; y < 2; ++y)
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[y][i] = 0.f;
+      // keys of two products at a time, requested while the ones before are multiplied
+      bf16x8 k[2][2][2];
+      const auto read_keys = [&](int n) {
 #pragma unroll
-      for (int p = 0; p < NP; ++p) {
-        const bool in = ND % 2 == 0 || 2 * p + h < ND;
-        const int blk = in ? 2 * p + h : ND - 1;
-        u32x4 code[2];
-        float sc[2];
+        for (int p = 0; p < 2; ++p)
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          code[y] = *reinterpret_cast<const u32x4*>(at + M::kKeys + (blk * kStep + 32 * y + c) * 16);
-          const uint32_t byte = reinterpret_cast<const uint8_t*>(at + M::kScales)[blk * kStep + 32 * y + c];
-          sc[y] = in ? scale_value(byte) : 1.f;
-        }
+          for (int y = 0; y < 2; ++y)
+            k[n & 1][p][y] = *reinterpret_cast<const bf16x8*>(at + M::kKeys + ((2 * (2 * n + p) + h) * kStep + 32 * y + c) * 16);
+        hold_all();
+      };
+      read_keys(0);
 #pragma unroll
-        for (int w = 0; w < 4; ++w)
+      for (int n = 0; n < NP / 2; ++n) {
+        if (n + 1 < NP / 2) read_keys(n + 1);
 #pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            const bf16x8 k = __builtin_bit_cast(bf16x8, eight_values(code[y][w], sc[y]));
+        for (int p = 0; p < 2; ++p)
 #pragma unroll
-            for (int t = 0; t < QT; ++t) s[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[p][w][t], s[y], 0, 0, 0);
-          }
+          for (int t = 0; t < QT; ++t)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) s[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[n & 1][p][y], q[2 * n + p][t], s[y], 0, 0, 0);
       }
       if (rarely(key + kStep - 1 > wave_low || there != 15)) {
         keep_branch();
@@ -392,6 +357,19 @@ __global__ __launch_bounds__(kThreads, ND <= 4 ? 2 : 1) void prompt_kernel(Promp
             for (int i = 0; i < 16; ++i) o[d][i] = NAN;
           }
       }
+      // values of 16 tokens at a time, requested while the ones before are multiplied: the first ones before the exponentials
+      bf16x8 v[2][ND];
+      const auto read_values = [&](int n) {
+        const char* const va = at + M::kValues + vlane + 16 * n * M::kStride;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(va + 64 * d));
+          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(va + 64 * d + 8 * M::kStride));
+          v[n & 1][d] = __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+        if constexpr (kAhead) hold_lds();
+      };
+      if constexpr (kAhead) read_values(0);
       float top = s[0][0];
 #pragma unroll
       for (int y = 0; y < 2; ++y)
@@ -420,6 +398,7 @@ __global__ __launch_bounds__(kThreads, ND <= 4 ? 2 : 1) void prompt_kernel(Promp
       for (int y = 0; y < 2; ++y)
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
+          if (!kAhead || 2 * y + x < 3) read_values(2 * y + x + (kAhead ? 1 : 0));
           bf16x8 pf[PT];
 #pragma unroll
           for (int t = 0; t < PT; ++t) {
@@ -436,15 +415,10 @@ __global__ __launch_bounds__(kThreads, ND <= 4 ? 2 : 1) void prompt_kernel(Promp
             }
             pf[t] = __builtin_bit_cast(bf16x8, w);
           }
-          const char* const va = at + M::kValues + vlane + (32 * y + 16 * x) * M::kStride;
 #pragma unroll
-          for (int d = 0; d < ND; ++d) {
-            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(va + 64 * d));
-            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(va + 64 * d + 8 * M::kStride));
-            const bf16x8 v = __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+          for (int d = 0; d < ND; ++d)
 #pragma unroll
-            for (int t = 0; t < PT; ++t) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pf[t], o[d], 0, 0, 0);
-          }
+            for (int t = 0; t < PT; ++t) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[x][d], pf[t], o[d], 0, 0, 0);
         }
     }
     if (more) {
