@@ -33,6 +33,9 @@ struct Prompt {
   int* cuts;      // [workgroups][4]: the tile that a workgroup begins and does not end, and the one that ends it
 };
 
+// Waves a SIMD (workgroups a unit) that the registers leave.  (Three, with spills: 692 us on long contexts where two take 375.)
+__host__ __device__ constexpr int prompt_waves(int nd) { return nd > 4 ? 1 : 2; }
+
 template <int ND>
 struct Lds {  // of one step
   static constexpr int kStride = 64 * (ND | 1);  // bytes of a token's values: four tokens lie in distinct banks
@@ -100,13 +103,15 @@ __device__ __forceinline__ void store_rows(const KvAttend& a, const f32x16 (&o)[
 }
 
 template <class X, int ND>
-__global__ __launch_bounds__(kThreads, ND <= 4 ? 2 : 1) void prompt_kernel(Prompt f) {
+__global__ __launch_bounds__(kThreads, prompt_waves(ND)) void prompt_kernel(Prompt f) {
   constexpr bool F = sizeof(typename X::storage) == 4;
   constexpr int QT = F ? 3 : 1, PT = F ? 3 : 1, NP = 2 * ND, KU = (ND + 3) / 4;
   using M = Lds<ND>;
-  // One wave a SIMD: nothing else hides what a read of LDS takes.  (ND <= 4: registers for it are dearer, us with / without 419 / 408 on long contexts; heads
-  // of 256, 2048 tokens x 16 heads: 111 / 123)
-  constexpr bool kAhead = ND > 4;
+  // 32 keys' scores at a time where the registers of 64 do not fit: fp32 rows, whose queries take three times the registers (2048 tokens x 32
+  // heads x 128: 144 us, in one piece 180), and wide heads (bf16, 2048 x 16 x 256: 118 us, in one piece 132)
+  constexpr int NY = F || ND > 6 ? 1 : 2;
+  // Values are requested ahead where registers are left for it
+  constexpr bool kAhead = !F || ND > 4;
   extern __shared__ __align__(16) char lds[];
   __shared__ Prefix prefix;
   __shared__ int spoiled[3][ND];  // first token of a step whose value is NaN, by block: three steps' worth, one of them being cleared
@@ -311,20 +316,22 @@ __global__ __launch_bounds__(kThreads, ND <= 4 ? 2 : 1) void prompt_kernel(Promp
     if ((int)threadIdx.x < ND) spoiled[(step + 2) % 3][threadIdx.x] = 0x7fffffff;
     const char* const at = lds + (step & 1) * M::kSize;
     const int key = step * kStep;
-    if (key <= wave_high) {  // else no row of this wave sees the step
-      f32x16 s[2];
 #pragma unroll
-      for (int y = 0; y < 2; ++y)
+    for (int y0 = 0; y0 < 2; y0 += NY) {
+      if (key + 32 * y0 > wave_high) continue;  // no row of this wave sees these keys
+      f32x16 s[NY];
+#pragma unroll
+      for (int y = 0; y < NY; ++y)
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[y][i] = 0.f;
       // keys of two products at a time, requested while the ones before are multiplied
-      bf16x8 k[2][2][2];
+      bf16x8 k[2][2][NY];
       const auto read_keys = [&](int n) {
 #pragma unroll
         for (int p = 0; p < 2; ++p)
 #pragma unroll
-          for (int y = 0; y < 2; ++y)
-            k[n & 1][p][y] = *reinterpret_cast<const bf16x8*>(at + M::kKeys + ((2 * (2 * n + p) + h) * kStep + 32 * y + c) * 16);
+          for (int y = 0; y < NY; ++y)
+            k[n & 1][p][y] = *reinterpret_cast<const bf16x8*>(at + M::kKeys + ((2 * (2 * n + p) + h) * kStep + 32 * (y0 + y) + c) * 16);
         hold_all();
       };
       read_keys(0);
@@ -336,31 +343,12 @@ __global__ __launch_bounds__(kThreads, ND <= 4 ? 2 : 1) void prompt_kernel(Promp
 #pragma unroll
           for (int t = 0; t < QT; ++t)
 #pragma unroll
-            for (int y = 0; y < 2; ++y) s[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[n & 1][p][y], q[2 * n + p][t], s[y], 0, 0, 0);
-      }
-      if (rarely(key + kStep - 1 > wave_low || there != 15)) {
-        keep_branch();
-#pragma unroll
-        for (int y = 0; y < 2; ++y)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int t = 32 * y + 8 * (i / 4) + 4 * h + i % 4;
-            s[y][i] = key + t <= lim && (there >> (2 * y + i / 8) & 1) ? s[y][i] : -INFINITY;
-          }
-      }
-      if (rarely(key + kStep - 1 > low || there != 15)) {  // as stage() has it
-        keep_branch();
-#pragma unroll
-        for (int d = 0; d < ND; ++d)
-          if (spoiled[step % 3][d] <= lim) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[d][i] = NAN;
-          }
+            for (int y = 0; y < NY; ++y) s[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[n & 1][p][y], q[2 * n + p][t], s[y], 0, 0, 0);
       }
       // values of 16 tokens at a time, requested while the ones before are multiplied: the first ones before the exponentials
       bf16x8 v[2][ND];
       const auto read_values = [&](int n) {
-        const char* const va = at + M::kValues + vlane + 16 * n * M::kStride;
+        const char* const va = at + M::kValues + vlane + (32 * y0 + 16 * n) * M::kStride;
 #pragma unroll
         for (int d = 0; d < ND; ++d) {
           const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(va + 64 * d));
@@ -370,9 +358,28 @@ __global__ __launch_bounds__(kThreads, ND <= 4 ? 2 : 1) void prompt_kernel(Promp
         if constexpr (kAhead) hold_lds();
       };
       if constexpr (kAhead) read_values(0);
+      if (rarely(key + 32 * (y0 + NY) - 1 > wave_low || there != 15)) {
+        keep_branch();
+#pragma unroll
+        for (int y = 0; y < NY; ++y)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int t = 32 * (y0 + y) + 8 * (i / 4) + 4 * h + i % 4;
+            s[y][i] = key + t <= lim && (there >> (2 * (y0 + y) + i / 8) & 1) ? s[y][i] : -INFINITY;
+          }
+      }
+      if (y0 == 0 && rarely(key + kStep - 1 > low || there != 15)) {  // as stage() has it
+        keep_branch();
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+          if (spoiled[step % 3][d] <= lim) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] = NAN;
+          }
+      }
       float top = s[0][0];
 #pragma unroll
-      for (int y = 0; y < 2; ++y)
+      for (int y = 0; y < NY; ++y)
 #pragma unroll
         for (int i = 0; i < 16; ++i) top = fmaxf(top, s[y][i]);
       if (__any(top * zscale > m + kSlack)) {
@@ -388,38 +395,38 @@ __global__ __launch_bounds__(kThreads, ND <= 4 ? 2 : 1) void prompt_kernel(Promp
       }
       const float base = m == -INFINITY ? 0.f : m;
 #pragma unroll
-      for (int y = 0; y < 2; ++y)
+      for (int y = 0; y < NY; ++y)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           s[y][i] = __builtin_amdgcn_exp2f(fmaf(s[y][i], zscale, -base));
           l += s[y][i];
         }
 #pragma unroll
-      for (int y = 0; y < 2; ++y)
+      for (int n = 0; n < 2 * NY; ++n) {
+        if constexpr (!kAhead) read_values(n);
+        else if (n + 1 < 2 * NY) read_values(n + 1);
+        float e[8];
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          if (!kAhead || 2 * y + x < 3) read_values(2 * y + x + (kAhead ? 1 : 0));
-          bf16x8 pf[PT];
+        for (int i = 0; i < 8; ++i) e[i] = s[n / 2][8 * (n & 1) + i];
+        bf16x8 pf[PT];
 #pragma unroll
-          for (int t = 0; t < PT; ++t) {
-            u32x4 w;
+        for (int t = 0; t < PT; ++t) {
+          u32x4 w;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              float& lo = reinterpret_cast<float*>(&s[y])[8 * x + 2 * i];
-              float& hi = reinterpret_cast<float*>(&s[y])[8 * x + 2 * i + 1];
-              w[i] = bf16_pair(lo, hi);
-              if (t + 1 < PT) {
-                lo -= bf16_lo(w[i]);
-                hi -= bf16_hi(w[i]);
-              }
+          for (int i = 0; i < 4; ++i) {
+            w[i] = bf16_pair(e[2 * i], e[2 * i + 1]);
+            if (t + 1 < PT) {
+              e[2 * i] -= bf16_lo(w[i]);
+              e[2 * i + 1] -= bf16_hi(w[i]);
             }
-            pf[t] = __builtin_bit_cast(bf16x8, w);
           }
-#pragma unroll
-          for (int d = 0; d < ND; ++d)
-#pragma unroll
-            for (int t = 0; t < PT; ++t) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[x][d], pf[t], o[d], 0, 0, 0);
+          pf[t] = __builtin_bit_cast(bf16x8, w);
         }
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+          for (int t = 0; t < PT; ++t) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[n & 1][d], pf[t], o[d], 0, 0, 0);
+      }
     }
     if (more) {
       stage(step + 1, next);
@@ -491,7 +498,7 @@ __global__ __launch_bounds__(kThreads) void join_tiles(Prompt f) {
 int64_t prompt_slots(const KvAttend& a) { return ceil_div(a.T * (a.heads / a.c.heads), kTile) + a.B; }
 
 // Workgroups that are resident at once: two a unit, one where a wave has more than half the registers.
-int prompt_resident(const KvAttend& a) { return a.c.dim <= 128 ? 512 : 256; }
+int prompt_resident(const KvAttend& a) { return 256 * prompt_waves(a.c.dim / 32); }
 // Whether the keys of all tiles are dealt out in equal shares: where tiles by themselves would leave workgroups idle, or are long enough that the parts of
 // cut tiles cost little beside them (in steps; each workgroup's two parts are written, read and joined).  us a call, shares / whole tiles: six ragged
 // fp32 prompts of 90 to 700 tokens, 24 heads over 8 of 96, 90 / 143; chunks of 512 tokens behind up to 15000 keys 410 / 472; 2048
