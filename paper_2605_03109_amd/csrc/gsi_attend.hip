@@ -16,7 +16,12 @@ namespace {
 constexpr int kWaves = 4, kThreads = kWaves * kWave;
 constexpr int kStep = 64;             // keys of a wave and step: the unit in which the work is dealt out
 constexpr int kPStride = kStep + 4;   // bf16 weights of a row in LDS
-constexpr int kManyParts = 12;        // parts of a tile that one wave joins by itself
+// Parts of a tile that one wave joins by itself: two contexts of 60000 and 131000 keys x 8 heads x 128, whose tiles have about 100 parts, take 55 us
+// with the four waves of a workgroup at them, 61 without; tiles of two or three parts do as well by single waves.
+constexpr int kManyParts = 12;
+// Workgroups of a launch, two a unit: 64 fp32 tokens x 32 heads over 287 MB 70.5 us, with 768 72.6 and with 1024 82 (more waves at
+// work on the memory at once, but more cut tiles and first loads).
+constexpr int kFewGroups = 512;
 
 struct Few {
   KvAttend a;
@@ -31,7 +36,8 @@ struct Few {
 };
 
 // Tiles of a request and the steps of each (one where there are rows but no keys).  A tile counts as kTileCost units and one for every step: its
-// queries, first loads and output cost a wave about as much as so many steps.
+// queries, first loads and output cost a wave about as much as so many steps (64 fp32 tokens x 32 heads over 287 MB: 70 us; counted as none 86, as
+// four 71; the other calls here lie within 3 % of their best with two).
 constexpr int kTileCost = 2;
 struct Steps {
   int tiles, per_tile;
@@ -743,6 +749,8 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Few f) {
 }
 
 // The smallest tile that holds the rows of the longest request that is expected: 2 (fp32), 4 (bf16), 8 or 16.
+// Products and exponentials grow with it: single fp32 tokens of 64 requests x 32 heads, 100 to 4000 keys x 128, in tiles of 2 70 us, of 16 96 us; 3 to 5 bf16
+// tokens of 16 requests x 16 heads, up to 6000 keys x 256, in tiles of 8 49 us, of 16 71 us.
 int few_tile(const KvAttend& a, int64_t few) {
   const int64_t rows = std::min(std::min(a.max_q, a.T) * (a.heads / a.c.heads), few);
   if (a.dtype == GSI_F32 && rows <= 2) return 2;
@@ -752,12 +760,14 @@ int few_tile(const KvAttend& a, int64_t few) {
 int64_t few_tiles(const KvAttend& a, int tile_rows) {
   return a.B * ceil_div(std::min(a.max_q, a.T) * (a.heads / a.c.heads), tile_rows) * a.c.heads;
 }
-bool few_whole(const KvAttend& a, int) { return a.max_len <= 512; }
+// Whether a workgroup takes a whole tile, its waves a part of the keys each, and nothing is cut or joined: where there is one tile at most for each, and the
+// keys are so few that sharing them out saves less than the joining costs.  us a call, whole tiles / shares, bf16 single tokens, two heads to one of
+// keys: 8 tiles of up to 1024 keys x 128 14 / 18, 2048 17 / 19, 4096 24 / 20; 512 tiles of 1024 18 / 23, 2048 24 / 27, 4096 43 / 43;
+// 64 tiles x 256 of 1024 18 / 19, 2048 26 / 22; 1024 tiles of 1024 29 / 28, 8192 tiles of up to 512 261 / 80.
+bool few_whole(const KvAttend& a, int tile_rows) { return few_tiles(a, tile_rows) <= kFewGroups && a.max_len <= (a.c.dim > 128 ? 1024 : 2048); }
 int few_workgroups(const KvAttend& a, int tile_rows) {
-  const double tiles = (double)few_tiles(a, tile_rows);
-  if (few_whole(a, tile_rows)) return (int)std::max(1.0, std::min(tiles, 4096.0));
-  const double units = tiles * (double)ceil_div(a.max_len, kStep) / kWaves;
-  return (int)std::max(1.0, std::min(units, 512.0));
+  const double tiles = (double)few_tiles(a, tile_rows), steps = few_whole(a, tile_rows) ? 1.0 : (double)ceil_div(a.max_len, kStep) / kWaves;
+  return (int)std::max(1.0, std::min(tiles * steps, (double)kFewGroups));
 }
 
 template <class X, int NR>
@@ -811,22 +821,34 @@ hipError_t attend_few(const KvAttend& a, int64_t few, void* ws, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Which kernels a call takes.  Requests of at most kFewRows rows of a head of keys are cheaper where a workgroup has 16 rows; where no
-// request is expected to have more, those take all of them, and where the requests are about of one length, or few rows are
-// not expected at all, the others do.
-constexpr int64_t kFewRows = 32;
+// Which kernels a call takes, by the rows that its longest request has to a head of keys (tokens times heads that share it).  The workgroups of few rows
+// read the keys once for 16 rows, those of many rows once for 128 but with a step that costs them as much for 20 rows as for 128.
+// us a call, few / many rows, 8 heads of keys:
+//   up to 16 rows: few.  16 rows, 16 requests of up to 4000 keys x 128: bf16 35 / 47, fp32 41 / 75.
+//   up to 32: few, but for bf16 over short contexts of many requests, where few rows are cut and joined and many are not.  32 rows, 64 requests of up to
+//     4000 keys: x 64 62 / 77, x 128 76 / 82, x 256 169 / 238, fp32 x 128 106 / 200; of up to 700: bf16 x 128 47 / 27.
+//   up to 64: few where that makes a tile for each workgroup at most (64 rows, 8 requests of up to 4000: bf16 40 / 45, fp32 50 / 77), and for fp32 rows of 128
+//     and more, whose products are three (64 requests: x 128 174 / 218, x 256 699 / 1094; x 64 124 / 108).
+//   more: many (128 rows, 64 requests of up to 700: bf16 80 / 37, fp32 110 / 76).
+// A call of single tokens and prompts takes both kernels, each for its requests, where the mean request has few rows.  both / many rows: 63 single tokens
+// behind 100 to 4000 keys and a prompt of 128, 32 heads of keys, bf16 120 / 192, fp32 191 / 492; requests of 1 to 64 tokens, four heads to
+// one of keys (60 rows in the mean), bf16 87 / 61.
+constexpr int64_t kFewRows = 16, kBothRows = 32;
 enum Kernels { kFewOnly, kPromptOnly, kBoth };
 static Kernels kernels_of(const KvAttend& a) {
-  const int64_t most = std::min(a.max_q, a.T);
-  if (most * (a.heads / a.c.heads) <= kFewRows || a.B == 0) return kFewOnly;
-  return 2 * a.T >= a.B * most ? kPromptOnly : kBoth;
+  const int64_t group = a.heads / a.c.heads, rows = std::min(a.max_q, a.T) * group;
+  const bool f32 = a.dtype == GSI_F32, fit = few_tiles(a, kFewRows) <= kFewGroups;
+  const bool few = rows <= kFewRows || (rows <= 2 * kFewRows && (fit || f32 || a.c.dim > 128 || a.max_len > 1024)) ||
+                   (rows <= 4 * kFewRows && (fit || (f32 && a.c.dim >= 128)));
+  if (few || a.B == 0) return kFewOnly;
+  return a.T * group < (f32 ? 3 : 1) * kFewRows * a.B ? kBoth : kPromptOnly;
 }
 
 size_t kv_attention_workspace(const KvAttend& a) {
   switch (kernels_of(a)) {
     case kFewOnly: return attend_few_workspace(a, INT64_MAX);
     case kPromptOnly: return attend_prompt_workspace(a);
-    default: return attend_few_workspace(a, kFewRows) + attend_prompt_workspace(a);
+    default: return attend_few_workspace(a, kBothRows) + attend_prompt_workspace(a);
   }
 }
 
@@ -836,8 +858,8 @@ hipError_t kv_attention(const KvAttend& a, void* ws, hipStream_t s) {
     case kPromptOnly: return attend_prompt(a, 0, true, ws, s);
     default: break;
   }
-  if (hipError_t e = attend_few(a, kFewRows, ws, s); e != hipSuccess) return e;
-  return attend_prompt(a, kFewRows, false, static_cast<char*>(ws) + attend_few_workspace(a, kFewRows), s);
+  if (hipError_t e = attend_few(a, kBothRows, ws, s); e != hipSuccess) return e;
+  return attend_prompt(a, kBothRows, false, static_cast<char*>(ws) + attend_few_workspace(a, kBothRows), s);
 }
 
 }  // namespace gsi

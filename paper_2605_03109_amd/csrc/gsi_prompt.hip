@@ -33,7 +33,7 @@ struct Prompt {
   int* cuts;      // [workgroups][4]: the tile that a workgroup begins and does not end, and the one that ends it
 };
 
-// Waves a SIMD (workgroups a unit) that the registers leave.  (Three, with spills: 692 us on long contexts where two take 375.)
+// Waves a SIMD (workgroups a unit) that the registers leave.  (Three, with spills: 692 us on long contexts where two take 385.)
 __host__ __device__ constexpr int prompt_waves(int nd) { return nd > 4 ? 1 : 2; }
 
 template <int ND>
@@ -499,13 +499,20 @@ int64_t prompt_slots(const KvAttend& a) { return ceil_div(a.T * (a.heads / a.c.h
 
 // Workgroups that are resident at once: two a unit, one where a wave has more than half the registers.
 int prompt_resident(const KvAttend& a) { return 256 * prompt_waves(a.c.dim / 32); }
-// Whether the keys of all tiles are dealt out in equal shares: where tiles by themselves would leave workgroups idle, or are long enough that the parts of
-// cut tiles cost little beside them (in steps; each workgroup's two parts are written, read and joined).  us a call, shares / whole tiles: six ragged
-// fp32 prompts of 90 to 700 tokens, 24 heads over 8 of 96, 90 / 143; chunks of 512 tokens behind up to 15000 keys 410 / 472; 2048
-// tokens x 32 heads x 128 from the first on, a tile for every workgroup, 81 / 70.
+// Whether the keys of all tiles are dealt out in equal shares.  That writes, reads and joins two parts a workgroup, about 15 us; whole tiles leave units idle: by
+// far the most where there are fewer tiles than workgroups fit, some where the tiles of about one round differ in length, little
+// after two rounds, whose last tiles are the shortest of a request.  Steps are weighted by what one costs (elements of a head, the three products of fp32).
+// us a call, shares / whole tiles, 8 heads of keys x 128, four heads to one, unless said:
+//   load below 0.75: 512 tokens after 3000, bf16 66 / 89, fp32 115 / 196; 256 after 2000 47 / 63; 60 after 15000 72 / 352; 1024 from the first on 49 / 34
+//   below 1.75: 8192 x 8 heads from the first on 175 / 199, 2048 x 32 heads 77 / 61 (its fp32 139 / 143); 2048 after 2000, tiles of about one
+//     length, 138 / 121; six of 300 after 100 to 3000 80 / 99; four of 512 after 6000 to 15000 383 / 432
+//   above: 4096 x 32 181 / 164; two of 8192 x 16 625 / 582; eight of 512 after 6000 to 15000 734 / 803, after 1500 to 4000 236 / 247, fp32 546 / 583; eight
+//     of 500 to 1000 after 500 to 3000 230 / 213
 bool prompt_shares(const KvAttend& a) {
   const double tiles = (double)a.c.heads * (double)ceil_div(a.T * (a.heads / a.c.heads), kTile), resident = prompt_resident(a);
-  return a.max_len > 16 * kStep && (tiles < 0.75 * resident || tiles * (double)a.max_len / kStep > 48.0 * resident);
+  const double load = tiles / resident, steps = (double)ceil_div(a.max_len, kStep) * (a.dtype == GSI_F32 ? 2 : 1) * a.c.dim / 128;
+  const double least = a.B == 1 ? steps * (double)std::max<int64_t>(a.max_len - a.T, 0) / (double)a.max_len : 0.0;  // of the shortest tile
+  return load < 0.75 ? steps >= 32.0 : load < 1.75 ? steps - least >= 48.0 : a.B > 1 && steps >= 64.0 * load;
 }
 size_t parts_bytes(const KvAttend& a, size_t W) { return 2 * W * kTile * a.c.dim * sizeof(float); }
 size_t stats_bytes(size_t W) { return 2 * W * kTile * sizeof(float2); }
@@ -555,6 +562,7 @@ hipError_t attend_prompt(const KvAttend& a, int64_t few, bool zero, void* ws, hi
   const size_t es = elem_size(a.dtype);
   f.q_wide = reinterpret_cast<uintptr_t>(a.Q) % 16 == 0 && (size_t)a.q_stride * es % 16 == 0;
   f.zero = zero;
+  // (2048 tokens x 32 heads x 128 61 us, without 64; two of 1500 x 32 heads x 64, whose workgroups are not all resident, 53 us, without 47)
   f.fold = prompt_slots(a) * a.c.heads <= prompt_resident(a) + a.B * a.c.heads;
   if (prompt_shares(a)) {
     const size_t W = prompt_resident(a);
