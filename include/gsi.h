@@ -347,9 +347,10 @@ typedef struct gsi_kv_cache {
  *   slots[t], positions[t] of the step's tokens t < q_start[B], -1 for the rest of T;
  *   status[0] = pages taken, status[1] = pages that were wanted and not there (none free, or the table too narrow): their
  *   entries and their tokens' slots are -1.
- * Negative lengths count as 0; where the step has more than T tokens, the last are dropped from the requests' n_new.
+ * Negative lengths count as 0, lengths above 2^30 as that many; T is at most 2^29.  Where the step has more than T tokens,
+ * the last are dropped from the requests' n_new.  B = 0: nothing is written.
  * kv_len, n_new and free_pages are not changed: the caller's free list begins status[0] entries later.  No output may lie over an
- * input.  The same call again gives the same results (the table's new entries are written again). */
+ * input (refused).  The same call again gives the same results (the table's new entries are written again). */
 int gsi_kv_tables(const int32_t* kv_len, const int32_t* n_new, int64_t B, const int32_t* free_pages, const int32_t* n_free,
                   int64_t free_cap, int32_t* table, int64_t width, int64_t page, int64_t T, int32_t* kv_len_out, int32_t* q_start,
                   int32_t* slots, int32_t* positions, int32_t* status, void* stream);

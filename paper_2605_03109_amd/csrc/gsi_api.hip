@@ -1909,9 +1909,10 @@ static int check_cache(const char* fn, const gsi_kv_cache* c, gsi::KvView& v) {
   v = gsi::KvView{c->K, c->K_scale, c->V, c->V_scale, c->n_pages, c->heads, c->dim, __builtin_ctz((unsigned)c->page)};
   return GSI_OK;
 }
+constexpr int64_t kMostGroups = (1 << 24) - 1;  // workgroups of 256 threads that one launch takes
 static int check_tokens(const char* fn, int64_t T, int64_t row) {
   if (T < 0 || T > (1ll << 30)) return fail(GSI_ERR_SHAPE, "%s: need 0 <= T <= 2^30, got %lld", fn, (long long)T);
-  if (gsi::ceil_div(T, 16) * gsi::ceil_div(row, 128) > 0x7fffffffll) return fail(GSI_ERR_SHAPE, "%s: too many tokens for one launch", fn);
+  if (gsi::ceil_div(T, 16) * gsi::ceil_div(row, 128) > kMostGroups) return fail(GSI_ERR_SHAPE, "%s: too many tokens for one launch", fn);
   return GSI_OK;
 }
 
@@ -1921,7 +1922,8 @@ int gsi_kv_tables(const int32_t* kv_len, const int32_t* n_new, int64_t B, const 
   const char* fn = "gsi_kv_tables";
   if (B < 0 || B > gsi::kKvMaxRequests)
     return fail(GSI_ERR_SHAPE, "%s: need 0 <= B <= %lld, got %lld", fn, (long long)gsi::kKvMaxRequests, (long long)B);
-  if (T < 0 || T > (1ll << 30)) return fail(GSI_ERR_SHAPE, "%s: need 0 <= T <= 2^30, got %lld", fn, (long long)T);
+  // (the sum of a length, taken as 2^30 at most, and of a step's tokens is an int)
+  if (T < 0 || T > (1ll << 29)) return fail(GSI_ERR_SHAPE, "%s: need 0 <= T <= 2^29, got %lld", fn, (long long)T);
   if (page < 16 || page > gsi::kKvMaxPage || (page & (page - 1)))
     return fail(GSI_ERR_SHAPE, "%s: page is a power of two in 16 .. %d, got %lld", fn, gsi::kKvMaxPage, (long long)page);
   if (width < 1 || width > (1ll << 30)) return fail(GSI_ERR_SHAPE, "%s: need 1 <= width <= 2^30, got %lld", fn, (long long)width);
@@ -1937,11 +1939,18 @@ int gsi_kv_tables(const int32_t* kv_len, const int32_t* n_new, int64_t B, const 
   if (T > 0) GSI_REQUIRE_PTR(slots);
   if (T > 0) GSI_REQUIRE_PTR(positions);
   GSI_REQUIRE_PTR(status);
-  for (const void* p : {(const void*)kv_len, (const void*)n_new, (const void*)free_pages, (const void*)n_free, (const void*)table,
-                        (const void*)kv_len_out, (const void*)q_start, (const void*)slots, (const void*)positions, (const void*)status})
-    if (!aligned(p, 4)) return fail(GSI_ERR_ALIGN, "%s: a pointer is not 4-byte aligned", fn);
-  if (kv_len_out == kv_len || kv_len_out == n_new)
-    return fail(GSI_ERR_SHAPE, "%s: kv_len_out lies over an input: workgroups read the lengths while others write", fn);
+  const struct { const void* p; int64_t n; } in[] = {{kv_len, B}, {n_new, B}, {free_pages, free_cap}, {n_free, 1}},
+                                             out[] = {{table, B * width}, {kv_len_out, B}, {q_start, B + 1}, {slots, T}, {positions, T}, {status, 2}};
+  for (const auto& x : in)
+    if (!aligned(x.p, 4)) return fail(GSI_ERR_ALIGN, "%s: a pointer is not 4-byte aligned", fn);
+  for (const auto& y : out) {
+    if (!aligned(y.p, 4)) return fail(GSI_ERR_ALIGN, "%s: a pointer is not 4-byte aligned", fn);
+    for (const auto& x : in) {
+      const uintptr_t a = reinterpret_cast<uintptr_t>(x.p), b = reinterpret_cast<uintptr_t>(y.p);
+      if (x.n > 0 && y.n > 0 && a < b + 4 * (uintptr_t)y.n && b < a + 4 * (uintptr_t)x.n)
+        return fail(GSI_ERR_SHAPE, "%s: an output lies over an input: workgroups read the inputs while others write", fn);
+    }
+  }
   hipError_t e = gsi::kv_tables(kv_len, n_new, B, free_pages, n_free, free_cap, table, width, __builtin_ctzll((unsigned long long)page), T,
                                 kv_len_out, q_start, slots, positions, status, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? GSI_OK : hip_fail(e, fn);
@@ -1994,6 +2003,7 @@ static int check_attend(const char* fn, const gsi_kv_cache* cache, int64_t T, in
   if (T < 0 || T > (1ll << 30) || B < 0 || B > (1ll << 20))
     return fail(GSI_ERR_SHAPE, "%s: need 0 <= T <= 2^30 and 0 <= B <= 2^20, got %lld and %lld", fn, (long long)T, (long long)B);
   if (T * (heads / a.c.heads) > (1ll << 30)) return fail(GSI_ERR_SHAPE, "%s: more than 2^30 rows of a head of keys", fn);
+  if ((gsi::ceil_div(T * (heads / a.c.heads), 128) + B) * a.c.heads > kMostGroups) return fail(GSI_ERR_SHAPE, "%s: too many tiles for one launch", fn);
   if (max_q < 1 || max_len < 1) return fail(GSI_ERR_SHAPE, "%s: need max_q >= 1 and max_len >= 1", fn);
   a.T = T;
   a.heads = (int)heads;

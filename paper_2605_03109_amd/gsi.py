@@ -563,6 +563,16 @@ def _i32(name: str, t: torch.Tensor, n: Optional[int] = None) -> int:
     return _ptr(t)
 
 
+def _empty(shape, dtype: torch.dtype, device, stream) -> torch.Tensor:
+    """An output, allocated on the stream that writes it: memory that another stream gave back may still be read there."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(stream.cuda_stream)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _rows_of_heads(name: str, t: torch.Tensor, dim: int) -> Tuple[int, int]:
     """(pointer, elements between tokens) of t[T, heads, dim] whose tokens may lie further apart than a row."""
     if not t.is_cuda:
@@ -579,10 +589,11 @@ def kv_tables(kv_len: torch.Tensor, n_new: torch.Tensor, free_pages: torch.Tenso
     B = kv_len.numel()
     if table.dim() != 2 or table.shape[0] != B:
         raise ValueError(f"table must be [{B}, width], got {tuple(table.shape)}")
-    out = torch.empty((2 * B + 1 + 2 * T + 2,), dtype=torch.int32, device=table.device)
-    new_len, start, slots, positions, status = out.split((B, B + 1, T, T, 2))
-    if B == 0:
-        start.zero_(), slots.fill_(-1), positions.fill_(-1), status.zero_()
+    out = _empty((2 * B + 1 + 2 * T + 2,), torch.int32, table.device, stream)
+    new_len, start, slots, positions, status = torch.unsafe_split_with_sizes(out, (B, B + 1, T, T, 2))  # (no views: 1.4 us, split 2.7)
+    if B == 0:  # the call does nothing then
+        with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) or stream is None else torch.cuda.ExternalStream(stream.cuda_stream)):
+            start.zero_(), slots.fill_(-1), positions.fill_(-1), status.zero_()
     base = out.data_ptr()
     _check(lib.gsi_kv_tables(_i32("kv_len", kv_len), _i32("n_new", n_new, B), B, _i32("free_pages", free_pages), _i32("n_free", n_free, 1),
                              free_pages.numel(), _i32("table", table), table.shape[1], page, T, base, base + 4 * B,
@@ -602,8 +613,8 @@ def kv_append(cache: KvCache, K: torch.Tensor, V: torch.Tensor, slots: torch.Ten
 def kv_expand(cache: KvCache, slots: torch.Tensor, dtype: torch.dtype = torch.float32, K=None, V=None, stream=None):
     """The values that the cache holds at slots[T]: K, V[T, heads, dim] in `dtype`; zero rows for negative slots."""
     shape = (slots.numel(), cache.heads, cache.dim)
-    K = torch.empty(shape, dtype=dtype, device=slots.device) if K is None else K
-    V = torch.empty(shape, dtype=dtype, device=slots.device) if V is None else V
+    K = _empty(shape, dtype, slots.device, stream) if K is None else K
+    V = _empty(shape, dtype, slots.device, stream) if V is None else V
     if tuple(K.shape) != shape or tuple(V.shape) != shape or K.dtype != V.dtype:
         raise ValueError(f"K and V must be {shape} of one dtype")
     _check(lib.gsi_kv_expand(ctypes.byref(cache.desc), _i32("slots", slots), slots.numel(), _ptr(K), _ptr(V), dtype_code(K), _stream(stream)))
@@ -623,11 +634,11 @@ def kv_attention(cache: KvCache, Q: torch.Tensor, q_start: Optional[torch.Tensor
     if table.dim() != 2 or table.shape[0] != B:
         raise ValueError(f"table must be [{B}, width], got {tuple(table.shape)}")
     qp, qs = _rows_of_heads("Q", Q, dim)
-    O = torch.empty((T, heads, dim), dtype=Q.dtype, device=Q.device) if O is None else O
+    O = _empty((T, heads, dim), Q.dtype, Q.device, stream) if O is None else O
     if tuple(O.shape) != (T, heads, dim) or O.dtype != Q.dtype:
         raise ValueError("O must have Q's shape and dtype")
     if lse is True:
-        lse = torch.empty((T, heads), dtype=torch.float32, device=Q.device)
+        lse = _empty((T, heads), torch.float32, Q.device, stream)
     elif lse is False:
         lse = None
     if lse is not None and (tuple(lse.shape) != (T, heads) or lse.dtype != torch.float32):
