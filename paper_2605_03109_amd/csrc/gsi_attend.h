@@ -49,6 +49,19 @@ __device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {  // both at le
   return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
 }
 
+// Quotients of numbers from 0 to below 2^31 by a divisor that the host knows.  m = floor(2^(31 + s) / d) + 1 with 2^s >= d is off by less than 2^s / d from
+// 2^(31 + s) / d, and the quotient by less than 1 / d.
+struct Divisor {
+  uint32_t m;
+  int shift;
+  Divisor() : Divisor(1) {}
+  explicit Divisor(uint32_t d) : shift(31) {
+    while ((1ull << (shift - 31)) < d) ++shift;
+    m = (uint32_t)((1ull << shift) / d + 1);
+  }
+  __device__ __forceinline__ int operator()(int x) const { return (int)(((uint64_t)(uint32_t)x * m) >> shift); }
+};
+
 // Work in units, by request: `units` says how many a span has.  The spans of 256 requests at a time and prefix sums of their units lie in LDS; all
 // threads of a workgroup of 256 call these functions together.
 constexpr int kScan = 256;
@@ -69,11 +82,12 @@ __device__ __forceinline__ int64_t scan_requests(const KvAttend& a, int64_t b0, 
   }
 #pragma unroll
   for (int o = 1; o < kWave; o <<= 1) {
+    if (o >= a.B) break;  // (what a lane behind the last request has then is not used)
     const int64_t up = __shfl_up(v, o, kWave);
     if (lane >= o) v += up;
   }
   __syncthreads();
-  if (lane == kWave - 1) x.sums[wave] = v;
+  if (lane == max((int)min(a.B - b0 - wave * kWave, (int64_t)kWave), 1) - 1) x.sums[wave] = v;
   __syncthreads();
   int64_t total = 0;
 #pragma unroll
@@ -108,12 +122,9 @@ __device__ __forceinline__ Place place_of(const KvAttend& a, Prefix& x, int64_t 
   for (int64_t b0 = 0; b0 < a.B && carry < total; b0 += kScan) {
     const int64_t here = a.B <= kScan ? total : scan_requests(a, b0, x, units);
     if (!found && u < carry + here) {
-      int lo = 0, hi = kScan - 1;  // the first request whose inclusive sum is above u - carry
-      while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (x.incl[mid] > u - carry) hi = mid;
-        else lo = mid + 1;
-      }
+      int lo = 0;  // the first request whose inclusive sum is above u - carry: behind all whose sums are not
+      for (int i = threadIdx.x % kWave; b0 + i - i % kWave < a.B && i < kScan; i += kWave)
+        lo += __popcll(__ballot(b0 + i < a.B && x.incl[i] <= u - carry));
       p.b = (int)b0 + lo;
       p.before = carry + (lo ? x.incl[lo - 1] : 0);
       found = true;

@@ -19,15 +19,13 @@ constexpr int kPStride = kStep + 4;   // bf16 weights of a row in LDS
 // Parts of a tile that one wave joins by itself: two contexts of 60000 and 131000 keys x 8 heads x 128, whose tiles have about 100 parts, take 55 us
 // with the four waves of a workgroup at them, 61 without; tiles of two or three parts do as well by single waves.
 constexpr int kManyParts = 12;
-// Workgroups of a launch, two a unit: 64 fp32 tokens x 32 heads over 287 MB 70.5 us, with 768 72.6 and with 1024 82 (more waves at
-// work on the memory at once, but more cut tiles and first loads).
-constexpr int kFewGroups = 512;
 
 struct Few {
   KvAttend a;
   int64_t few;    // requests of more rows are another kernel's
   int group;      // heads that share a head of keys
   int tile_rows;  // rows of a tile
+  Divisor by_group, by_heads, by_tile;  // by the heads of a group, the heads of keys, the rows of a tile
   int q_wide;     // 16-byte loads of queries
   int whole;      // a workgroup takes whole tiles, its waves parts of their keys; else every wave an equal share of all steps
   float* parts;   // [2 * waves][tile_rows][dim]: sums of a cut tile
@@ -44,7 +42,7 @@ struct Steps {
 };
 __device__ __forceinline__ Steps steps_of(const Few& f, const Span& s) {
   const int64_t rows = (int64_t)s.n * f.group;
-  return Steps{rows <= f.few ? (int)((uint32_t)(rows + f.tile_rows - 1) / (uint32_t)f.tile_rows) : 0, max(1, (s.len + kStep - 1) / kStep)};
+  return Steps{rows <= f.few ? f.by_tile((int)rows + f.tile_rows - 1) : 0, max(1, (s.len + kStep - 1) / kStep)};
 }
 __device__ __forceinline__ int tile_units(const Few& f, const Steps& st) { return f.whole ? 1 : st.per_tile + kTileCost; }
 
@@ -177,8 +175,15 @@ struct Rows {
   __device__ static __forceinline__ int term(int x) { return kFold ? min(x % 4, 2) : 0; }
 };
 
+// Workgroups a unit that the registers leave.  (One where two would spill: 64 requests of 3 tokens behind up to 4000 keys x 256, 8 heads to one of keys,
+// bf16 149 us, with two and spills 204; fp32 210, 425.)
+__host__ __device__ constexpr int few_resident(bool f32, int tile_rows, int width) {
+  if (width > 128 && (tile_rows == 16 || (tile_rows == 8 && f32))) return 1;
+  return width > 128 || tile_rows > 4 ? 2 : 3;
+}
+
 template <class X, int NR, int DPL, bool EXACT>
-__global__ __launch_bounds__(kThreads, DPL == 16 || NR > 1 ? 2 : 3) void few_kernel(Few f) {
+__global__ __launch_bounds__(kThreads, few_resident(sizeof(typename X::storage) == 4, 4 * NR, 16 * DPL)) void few_kernel(Few f) {
   constexpr bool F = sizeof(typename X::storage) == 4;
   using R = Rows<F, NR>;
   using Ln = Lane<DPL>;
@@ -204,12 +209,13 @@ __global__ __launch_bounds__(kThreads, DPL == 16 || NR > 1 ? 2 : 3) void few_ker
     clear_idle_rows<X>(a);
     return;
   }
-  const Shares sh = shares_of(total, gridDim.x, kWaves);
+  Shares sh{};
   int64_t u, u_end;
   if (f.whole) {
     u = blockIdx.x;
     u_end = total;
   } else {
+    sh = shares_of(total, gridDim.x, kWaves);
     if (blockIdx.x >= sh.groups) {
       clear_idle_rows<X>(a);
       return;
@@ -266,9 +272,9 @@ __global__ __launch_bounds__(kThreads, DPL == 16 || NR > 1 ? 2 : 3) void few_ker
     sp.t0 = __builtin_amdgcn_readfirstlane(sp.t0);
     sp.n = __builtin_amdgcn_readfirstlane(sp.n);
     sp.len = __builtin_amdgcn_readfirstlane(sp.len);
-    const int seg = __builtin_amdgcn_readfirstlane((int)divide(u - before, per));
+    const int seg = __builtin_amdgcn_readfirstlane(f.whole ? (int)(u - before) : (int)divide(u - before, per));
     const int64_t seg_begin = before + (int64_t)seg * per;
-    const int tile = (int)((uint32_t)seg / (uint32_t)a.c.heads), kvh = seg - tile * a.c.heads;
+    const int tile = f.by_heads(seg), kvh = seg - tile * a.c.heads;
     const int rows = min(TR, sp.n * f.group - tile * TR);
     int first, last;  // steps
     if (f.whole) {
@@ -293,7 +299,7 @@ __global__ __launch_bounds__(kThreads, DPL == 16 || NR > 1 ? 2 : 3) void few_ker
     {
       const int r = R::row(L.c), rid = tile * TR + r;
       const bool real = r >= 0 && r < rows;
-      const int tok = real ? rid / f.group : 0, head = kvh * f.group + (real ? rid % f.group : 0);
+      const int tok = real ? f.by_group(rid) : 0, head = kvh * f.group + (real ? rid - tok * f.group : 0);
       const typename X::storage* const Q = reinterpret_cast<const typename X::storage*>(a.Q) + (int64_t)(sp.t0 + tok) * a.q_stride + (int64_t)head * D;
 #pragma unroll
       for (int x = 0; x < KW / 2; ++x) {
@@ -331,13 +337,13 @@ __global__ __launch_bounds__(kThreads, DPL == 16 || NR > 1 ? 2 : 3) void few_ker
     }
     // the last key that a row sees: by the layout of the scores, and of the output (the same but where terms are folded)
     int lim[NS], lim_o[NS];
-    const auto last_key = [&](int r) { return r < rows ? sp.len - sp.n + (tile * TR + r) / f.group : -1; };
+    const auto last_key = [&](int r) { return r < rows ? sp.len - sp.n + f.by_group(tile * TR + r) : -1; };
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
       lim[i] = last_key(L.g + 4 * i);
       lim_o[i] = R::kFold ? last_key(L.g / 2) : lim[i];
     }
-    const int lim_low = sp.len - sp.n + tile * TR / f.group;  // what every row of the tile sees
+    const int lim_low = sp.len - sp.n + f.by_group(tile * TR);  // what every row of the tile sees
 
     f32x4 o[NO][JP];
     float m[NS], l[NS];
@@ -614,7 +620,8 @@ __global__ __launch_bounds__(kThreads, DPL == 16 || NR > 1 ? 2 : 3) void few_ker
         const int r = 4 * i + L.g;
         if (!holds || r >= rows) continue;
         const int rid = tile * TR + r;
-        const int64_t orow = (int64_t)(sp.t0 + rid / f.group) * a.heads + kvh * f.group + rid % f.group;
+        const int tok = f.by_group(rid);
+        const int64_t orow = (int64_t)(sp.t0 + tok) * a.heads + kvh * f.group + rid - tok * f.group;
         if (complete) {
           const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
           typename X::storage* const to_o = reinterpret_cast<typename X::storage*>(a.O) + orow * D + DPL * L.c;
@@ -736,7 +743,8 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Few f) {
       }
       if ((many ? (int)threadIdx.x : lane) < lanes) {
         const int rid = tile * f.tile_rows + r;
-        const int64_t orow = (int64_t)(sp.t0 + rid / f.group) * a.heads + kvh * f.group + rid % f.group;
+        const int tok = f.by_group(rid);
+        const int64_t orow = (int64_t)(sp.t0 + tok) * a.heads + kvh * f.group + rid - tok * f.group;
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
         typename X::storage* const to = reinterpret_cast<typename X::storage*>(a.O) + orow * D + d;
         if (d < D)
@@ -760,14 +768,17 @@ int few_tile(const KvAttend& a, int64_t few) {
 int64_t few_tiles(const KvAttend& a, int tile_rows) {
   return a.B * ceil_div(std::min(a.max_q, a.T) * (a.heads / a.c.heads), tile_rows) * a.c.heads;
 }
+// Workgroups of a launch: two a unit, or one where no more are resident.  64 fp32 tokens x 32 heads over 287 MB 70.5 us, with 768 72.6 and with 1024 82 (more
+// waves at work on the memory at once, but more cut tiles and first loads); one a unit: those 3 tokens x 256 of bf16 128 us, with 512 149.
+int few_groups(const KvAttend& a, int tile_rows) { return 256 * std::min(few_resident(a.dtype == GSI_F32, tile_rows, a.c.dim), 2); }
 // Whether a workgroup takes a whole tile, its waves a part of the keys each, and nothing is cut or joined: where there is one tile at most for each, and the
 // keys are so few that sharing them out saves less than the joining costs.  us a call, whole tiles / shares, bf16 single tokens, two heads to one of
 // keys: 8 tiles of up to 1024 keys x 128 14 / 18, 2048 17 / 19, 4096 24 / 20; 512 tiles of 1024 18 / 23, 2048 24 / 27, 4096 43 / 43;
 // 64 tiles x 256 of 1024 18 / 19, 2048 26 / 22; 1024 tiles of 1024 29 / 28, 8192 tiles of up to 512 261 / 80.
-bool few_whole(const KvAttend& a, int tile_rows) { return few_tiles(a, tile_rows) <= kFewGroups && a.max_len <= (a.c.dim > 128 ? 1024 : 2048); }
+bool few_whole(const KvAttend& a, int tile_rows) { return few_tiles(a, tile_rows) <= few_groups(a, tile_rows) && a.max_len <= (a.c.dim > 128 ? 1024 : 2048); }
 int few_workgroups(const KvAttend& a, int tile_rows) {
   const double tiles = (double)few_tiles(a, tile_rows), steps = few_whole(a, tile_rows) ? 1.0 : (double)ceil_div(a.max_len, kStep) / kWaves;
-  return (int)std::max(1.0, std::min(tiles * steps, (double)kFewGroups));
+  return (int)std::max(1.0, std::min(tiles * steps, (double)few_groups(a, tile_rows)));
 }
 
 template <class X, int NR>
@@ -809,6 +820,9 @@ hipError_t attend_few(const KvAttend& a, int64_t few, void* ws, hipStream_t s) {
   f.few = few;
   f.group = a.heads / a.c.heads;
   f.tile_rows = few_tile(a, few);
+  f.by_group = Divisor(f.group);
+  f.by_heads = Divisor(a.c.heads);
+  f.by_tile = Divisor(f.tile_rows);
   f.whole = few_whole(a, f.tile_rows);
   const size_t es = elem_size(a.dtype);
   f.q_wide = reinterpret_cast<uintptr_t>(a.Q) % 16 == 0 && (size_t)a.q_stride * es % 16 == 0;
@@ -837,7 +851,7 @@ constexpr int64_t kFewRows = 16, kBothRows = 32;
 enum Kernels { kFewOnly, kPromptOnly, kBoth };
 static Kernels kernels_of(const KvAttend& a) {
   const int64_t group = a.heads / a.c.heads, rows = std::min(a.max_q, a.T) * group;
-  const bool f32 = a.dtype == GSI_F32, fit = few_tiles(a, kFewRows) <= kFewGroups;
+  const bool f32 = a.dtype == GSI_F32, fit = few_tiles(a, kFewRows) <= few_groups(a, kFewRows);
   const bool few = rows <= kFewRows || (rows <= 2 * kFewRows && (fit || f32 || a.c.dim > 128 || a.max_len > 1024)) ||
                    (rows <= 4 * kFewRows && (fit || (f32 && a.c.dim >= 128)));
   if (few || a.B == 0) return kFewOnly;

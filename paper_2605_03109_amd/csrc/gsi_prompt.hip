@@ -24,6 +24,7 @@ struct Prompt {
   KvAttend a;
   int64_t few;   // requests of at most so many rows are another kernel's
   int group;
+  Divisor by_group, by_heads;  // by the heads of a group, the heads of keys
   int q_wide;
   int zero;       // whether this launch clears the rows of tokens of no request
   int fold;       // whole tiles: of a request, the one half from the last on, then the other from the first on
@@ -49,7 +50,7 @@ __device__ __forceinline__ int64_t tiles_of(const Prompt& f, const Span& s) {
 }
 
 __device__ __forceinline__ int high_of(const Prompt& f, const Span& s, int tile) {  // the last key that a row of the tile sees
-  return s.len - s.n + (int)((uint32_t)min(tile * kTile + kTile - 1, s.n * f.group - 1) / (uint32_t)f.group);
+  return s.len - s.n + f.by_group(min(tile * kTile + kTile - 1, s.n * f.group - 1));
 }
 __device__ __forceinline__ int steps_of(const Prompt& f, const Span& s, int tile) { return max(0, high_of(f, s, tile)) / kStep + 1; }
 
@@ -127,12 +128,12 @@ __global__ __launch_bounds__(kThreads, prompt_waves(ND)) void prompt_kernel(Prom
   if (!f.parts) {
     // heads of keys run fastest: with eight of them and more, a cache holds the same ones throughout
     const auto units = [&](const Span& s) { return tiles_of(f, s); };
-    const int64_t total = total_units(a, prefix, units), slot = blockIdx.x / a.c.heads;
+    const int64_t total = total_units(a, prefix, units), slot = f.by_heads(blockIdx.x);
     const Place p = place_of(a, prefix, total, slot, units);
     if (f.zero) clear_idle_rows<X>(a);
     if (slot >= total) return;
     b = p.b;
-    kvh = blockIdx.x % a.c.heads;
+    kvh = (int)blockIdx.x - (int)slot * a.c.heads;
     const int64_t n = tiles_of(f, span_at(a, prefix, b)), i = slot - p.before;
     // The last tiles see the most keys and come first.  Where all workgroups are resident at once, a unit has the i-th and the i-th of the second
     // half: that half runs the other way, and what two workgroups of a unit do together is about the same everywhere.
@@ -199,13 +200,13 @@ __global__ __launch_bounds__(kThreads, prompt_waves(ND)) void prompt_kernel(Prom
 
   const int rid = row0 + 32 * wave + c;
   const bool real = rid < all_rows;
-  const int tok = real ? rid / f.group : 0, head = kvh * f.group + (real ? rid % f.group : 0);
+  const int tok = real ? f.by_group(rid) : 0, head = kvh * f.group + (real ? rid - tok * f.group : 0);
   const int lim = real ? shift0 + tok : -1;  // the last key that this lane's row sees
   // of the wave's rows, and of the workgroup's: the last key that any sees, and the last that all see (idle rows aside)
   const int wave_first = row0 + 32 * wave, wave_last = min(wave_first + 31, all_rows - 1);
-  const int wave_high = wave_first < all_rows ? shift0 + wave_last / f.group : -1;
-  const int wave_low = wave_first < all_rows ? shift0 + wave_first / f.group : -1;
-  const int low = shift0 + row0 / f.group;
+  const int wave_high = wave_first < all_rows ? shift0 + f.by_group(wave_last) : -1;
+  const int wave_low = wave_first < all_rows ? shift0 + f.by_group(wave_first) : -1;
+  const int low = shift0 + f.by_group(row0);
 
   // query rows: the operand's elements 8 h + u of product p are elements 16 p + 8 h + u
   bf16x8 q[NP][QT];
@@ -491,7 +492,8 @@ __global__ __launch_bounds__(kThreads) void join_tiles(Prompt f) {
     }
   }
   if (rid >= sp.n * f.group) return;
-  const int64_t orow = (int64_t)(sp.t0 + rid / f.group) * a.heads + kvh * f.group + rid % f.group;
+  const int tok = f.by_group(rid);
+  const int64_t orow = (int64_t)(sp.t0 + tok) * a.heads + kvh * f.group + rid - tok * f.group;
   store_rows<X, 1>(a, o, top, sum, orow, h, d);
 }
 
@@ -559,6 +561,8 @@ hipError_t attend_prompt(const KvAttend& a, int64_t few, bool zero, void* ws, hi
   f.a = a;
   f.few = few;
   f.group = a.heads / a.c.heads;
+  f.by_group = Divisor(f.group);
+  f.by_heads = Divisor(a.c.heads);
   const size_t es = elem_size(a.dtype);
   f.q_wide = reinterpret_cast<uintptr_t>(a.Q) % 16 == 0 && (size_t)a.q_stride * es % 16 == 0;
   f.zero = zero;
