@@ -853,7 +853,7 @@ static Kernels kernels_of(const KvAttend& a) {
   const int64_t group = a.heads / a.c.heads, rows = std::min(a.max_q, a.T) * group;
   const bool f32 = a.dtype == GSI_F32, fit = few_tiles(a, kFewRows) <= few_groups(a, kFewRows);
   const bool few = rows <= kFewRows || (rows <= 2 * kFewRows && (fit || f32 || a.c.dim > 128 || a.max_len > 1024)) ||
-                   (rows <= 4 * kFewRows && (fit || (f32 && a.c.dim >= 128)));
+                   (rows <= 4 * kFewRows && (fit || (f32 && a.c.dim >= 128) || a.c.dim > 192));
   if (few || a.B == 0) return kFewOnly;
   return a.T * group < (f32 ? 3 : 1) * kFewRows * a.B ? kBoth : kPromptOnly;
 }

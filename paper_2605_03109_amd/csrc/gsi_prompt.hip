@@ -108,11 +108,15 @@ __global__ __launch_bounds__(kThreads, prompt_waves(ND)) void prompt_kernel(Prom
   constexpr bool F = sizeof(typename X::storage) == 4;
   constexpr int QT = F ? 3 : 1, PT = F ? 3 : 1, NP = 2 * ND, KU = (ND + 3) / 4;
   using M = Lds<ND>;
-  // 32 keys' scores at a time where the registers of 64 do not fit: fp32 rows, whose queries take three times the registers (2048 tokens x 32
-  // heads x 128: 144 us, in one piece 180), and wide heads (bf16, 2048 x 16 x 256: 118 us, in one piece 132)
-  constexpr int NY = F || ND > 6 ? 1 : 2;
+  // fp32 queries of 224 elements and more are read again in every step: their three terms and the output would take all registers.  (2048 tokens x 16
+  // heads x 256 182 us, kept with spills 381; x 192, where they fit, 118, read again 152; x 128 at two workgroups a unit 91, 90 and in chunks
+  // behind long contexts 276, 318.)
+  constexpr bool kStream = F && ND > 6;
+  // 32 keys' scores at a time where the registers of 64 do not fit: fp32 rows that keep their queries (2048 tokens x 32 heads x 128: 139 us, in one
+  // piece 180), and wide heads (bf16, 2048 x 16 x 256: 103 us, in one piece 111)
+  constexpr int NY = (F && !kStream) || (!F && ND > 6) ? 1 : 2;
   // Values are requested ahead where registers are left for it
-  constexpr bool kAhead = !F || ND > 4;
+  constexpr bool kAhead = !F || ND == 5;
   extern __shared__ __align__(16) char lds[];
   __shared__ Prefix prefix;
   __shared__ int spoiled[3][ND];  // first token of a step whose value is NaN, by block: three steps' worth, one of them being cleared
@@ -209,9 +213,9 @@ __global__ __launch_bounds__(kThreads, prompt_waves(ND)) void prompt_kernel(Prom
   const int low = shift0 + f.by_group(row0);
 
   // query rows: the operand's elements 8 h + u of product p are elements 16 p + 8 h + u
-  bf16x8 q[NP][QT];
-  {
-    const typename X::storage* const Q = reinterpret_cast<const typename X::storage*>(a.Q) + (int64_t)(sp.t0 + tok) * a.q_stride + (int64_t)head * D;
+  const typename X::storage* Q = reinterpret_cast<const typename X::storage*>(a.Q) + (int64_t)(sp.t0 + tok) * a.q_stride + (int64_t)head * D;
+  bf16x8 q[kStream ? 2 : NP][QT];
+  if constexpr (!kStream) {
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
       QueryPart<X, 8> raw;
@@ -301,10 +305,12 @@ __global__ __launch_bounds__(kThreads, prompt_waves(ND)) void prompt_kernel(Prom
     there = r.there;
     stage(step0, r);
   }
+  if constexpr (!kStream) {
 #pragma unroll
-  for (int p = 0; p < NP; ++p)
+    for (int p = 0; p < NP; ++p)
 #pragma unroll
-    for (int t = 0; t < QT; ++t) arrive(q[p][t]);
+      for (int t = 0; t < QT; ++t) arrive(q[p][t]);
+  }
   __syncthreads();
   const int vlane = (4 * h + ((lane & 15) >> 2)) * M::kStride + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
   for (int step = step0; step < step1; ++step) {
@@ -327,7 +333,13 @@ __global__ __launch_bounds__(kThreads, prompt_waves(ND)) void prompt_kernel(Prom
         for (int i = 0; i < 16; ++i) s[y][i] = 0.f;
       // keys of two products at a time, requested while the ones before are multiplied
       bf16x8 k[2][2][NY];
+      QueryPart<X, 8> raw[2][2];
+      if constexpr (kStream) asm volatile("" : "+v"(Q));  // (not read once in front of all steps)
       const auto read_keys = [&](int n) {
+        if constexpr (kStream) {
+#pragma unroll
+          for (int p = 0; p < 2; ++p) raw[n & 1][p].load(Q, 16 * (2 * n + p) + 8 * h, real, f.q_wide, a.scale < 0.f);
+        }
 #pragma unroll
         for (int p = 0; p < 2; ++p)
 #pragma unroll
@@ -340,11 +352,13 @@ __global__ __launch_bounds__(kThreads, prompt_waves(ND)) void prompt_kernel(Prom
       for (int n = 0; n < NP / 2; ++n) {
         if (n + 1 < NP / 2) read_keys(n + 1);
 #pragma unroll
-        for (int p = 0; p < 2; ++p)
+        for (int p = 0; p < 2; ++p) {
+          if constexpr (kStream) raw[n & 1][p].template terms<QT>(0, q[p]);
 #pragma unroll
           for (int t = 0; t < QT; ++t)
 #pragma unroll
-            for (int y = 0; y < NY; ++y) s[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[n & 1][p][y], q[2 * n + p][t], s[y], 0, 0, 0);
+            for (int y = 0; y < NY; ++y) s[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[n & 1][p][y], q[kStream ? p : 2 * n + p][t], s[y], 0, 0, 0);
+        }
       }
       // values of 16 tokens at a time, requested while the ones before are multiplied: the first ones before the exponentials
       bf16x8 v[2][ND];
