@@ -373,7 +373,8 @@ int gsi_kv_expand(const gsi_kv_cache* cache, const int32_t* slots, int64_t T, vo
  * max_q, max_len: the most new tokens and keys that a request is expected to have.  They choose kernels and their launches; other
  * numbers cost time and never change what is computed.
  * Arithmetic: fp32 sums and statistics of bf16 products; keys and values are exact in bf16, queries and weights exp(s - max) enter in
- * one bf16 term (bf16: a query itself, a weight rounded once) or in three (fp32). ws: gsi_kv_attention_workspace_bytes(). */
+ * one bf16 term (bf16: a query itself, a weight rounded once; for up to four rows in two terms) or in three (fp32).
+ * ws: gsi_kv_attention_workspace_bytes(). */
 int gsi_kv_attention(const gsi_kv_cache* cache, const void* Q, int64_t T, int64_t heads, int64_t q_stride, int dtype,
                      const int32_t* q_start, const int32_t* kv_len, int64_t B, const int32_t* table, int64_t width, int64_t max_q,
                      int64_t max_len, float scale, void* O, float* lse, void* ws, size_t ws_bytes, void* stream);

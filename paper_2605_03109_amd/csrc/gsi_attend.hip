@@ -161,14 +161,17 @@ __device__ __forceinline__ void load_values(Values<DPL>& v, const KvAttend& a, c
 
 // Rows of the products.  Rows r of a tile lie in lane group r % 4 and register r / 4 of the scores.  FOLD: two rows of fp32, whose three terms (of a
 // query, of a weight) are rows of one product instead of three products: row r's terms are the registers of lane group r of the scores,
-// which are added, and the registers of lane groups 2 r and 2 r + 1 (even, odd elements) of the output, which are added at the end.
+// which are added, and the registers of lane groups 2 r and 2 r + 1 (even, odd elements) of the output, which are added at the end.  TWO: four rows of
+// bf16, whose weights have a second term in the rows of the second product that would be idle: the output is then off by its own rounding alone
+// (to 64 bits 0.0017 of it; with one term 0.0024).
 template <bool F, int NR>
 struct Rows {
   static constexpr bool kFold = F && NR == 0;
   static constexpr int kTile = kFold ? 2 : 4 * NR;      // rows of a tile
   static constexpr int kRegs = kFold ? 1 : NR;          // registers of scores
   static constexpr int kChain = F && !kFold ? 3 : 1;    // products that add up terms
-  static constexpr int kImages = F ? 3 : 1;             // of the weights in LDS
+  static constexpr bool kTwo = !F && NR == 1;
+  static constexpr int kImages = F ? 3 : kTwo ? 2 : 1;  // of the weights in LDS
   static constexpr int kOut = kRegs > 2 ? 2 : 1;        // products that share converted values
   // row of the tile, and term, that row x of the first product has (-1: none)
   __device__ static __forceinline__ int row(int x) { return kFold ? (x / 4 < 2 && x % 4 < 3 ? x / 4 : -1) : (x % 4 < NR ? x / 4 + 4 * (x % 4) : -1); }
@@ -249,7 +252,7 @@ __global__ __launch_bounds__(kThreads, few_resident(sizeof(typename X::storage) 
     p_odd = (L.c / 4) & 1;
   } else {
 #pragma unroll
-    for (int y = 0; y < NO; ++y) p_row[y] = (L.c / 4 + 4 * min(2 * y + (L.c % 4) / 2, NS - 1)) * kPStride;
+    for (int y = 0; y < NO; ++y) p_row[y] = R::kTwo ? (L.c % 4 / 2 * TR + L.c / 4) * kPStride : (L.c / 4 + 4 * min(2 * y + (L.c % 4) / 2, NS - 1)) * kPStride;
     p_odd = L.c & 1;
   }
   const uint32_t sel0 = p_odd ? 0x01000c0cu : 0x0c0c0100u, sel1 = p_odd ? 0x03020c0cu : 0x0c0c0302u;
@@ -357,8 +360,8 @@ __global__ __launch_bounds__(kThreads, few_resident(sizeof(typename X::storage) 
       l[i] = 0.f;
     }
     const auto scale_out = [&](const float (&by)[NS]) {  // by: of the lane's rows of scores
-      if constexpr (R::kFold) {
-        const float k = __shfl(by[0], (L.g / 2) * 16 + L.c, kWave);
+      if constexpr (R::kFold || R::kTwo) {
+        const float k = R::kFold ? __shfl(by[0], (L.g / 2) * 16 + L.c, kWave) : by[0];
 #pragma unroll
         for (int j = 0; j < JP; ++j) o[0][j] *= k;
       } else {
@@ -538,8 +541,8 @@ __global__ __launch_bounds__(kThreads, few_resident(sizeof(typename X::storage) 
       for (int i = 0; i < NS; ++i)
 #pragma unroll
         for (int j = 0; j < JP; ++j) {
-          out[i][2 * j] = o[i / 2][j][2 * (i % 2)];
-          out[i][2 * j + 1] = o[i / 2][j][2 * (i % 2) + 1];
+          out[i][2 * j] = R::kTwo ? o[0][j][0] + o[0][j][2] : o[i / 2][j][2 * (i % 2)];
+          out[i][2 * j + 1] = R::kTwo ? o[0][j][1] + o[0][j][3] : o[i / 2][j][2 * (i % 2) + 1];
         }
     }
     const bool holds = !R::kFold || L.g < TR;  // lane groups with rows
