@@ -4,7 +4,7 @@
 // outputs are kept transposed, tokens by rows and elements by rows: a row's scores then lie in two lanes, its maximum and its sum
 // need no exchange but one, and the weights are the second product's operand as they come out of the first (the tokens of its
 // contraction taken in the order of the accumulator's registers).  Keys and values are converted once, on their way to LDS; values are read
-// there with the transposing reads.  (By each wave for itself, chunks of 512 tokens behind 6000 to 15000 keys took 410 us, so 379.)
+// there with the transposing reads.  (By each wave for itself, chunks of 512 tokens behind 6000 to 15000 keys took 410 us; this way 379.)
 //
 // Issue bounds it: those chunks, 346 GFLOP, run at 0.91 PFLOP/s (a library product of 8192^3 at 1.2), with the matrix units busy for a third of the time;
 // exponentials, sums, the conversion of the next step and the reads of LDS take the slots of a SIMD's two waves beside them.  2048 tokens from the
