@@ -481,33 +481,45 @@ __global__ __launch_bounds__(kThreads, prompt_waves(ND)) void prompt_kernel(Prom
 }
 
 // Joins the parts of a cut tile in their order: a workgroup for each 32 elements of the tile that another has begun and not ended, whose threads
-// have the rows and elements that those of prompt_kernel had.  Memory bounds it: 512 workgroups' parts of 128 x 128, 64 MB, 17 us; of 128 x 96 15 us.
+// have the rows and elements that those of prompt_kernel had.  Memory bounds it: 512 workgroups' parts of 128 x 128, 64 MB, 17 us; of 128 x 96 14 us.
 template <class X>
 __global__ __launch_bounds__(kThreads) void join_tiles(Prompt f) {
   const KvAttend& a = f.a;
-  const int w = blockIdx.x, d = blockIdx.y, b = f.cuts[4 * w];
+  const int w = blockIdx.x, d = blockIdx.y;
+  typedef int i32x4 __attribute__((ext_vector_type(4)));
+  const i32x4 cut = *reinterpret_cast<const i32x4*>(f.cuts + 4 * w);
+  const int b = cut[0], tile = cut[1], kvh = cut[2], end = cut[3];
   if (b < 0) return;
-  const int tile = f.cuts[4 * w + 1], kvh = f.cuts[4 * w + 2], end = f.cuts[4 * w + 3];
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, c = lane & 31, h = lane >> 5;
   const Span sp = span_of(a, b);
   const int rid = tile * kTile + 32 * wave + c;
-  const auto place = [&](int i) -> int64_t { return i == w ? 2 * i + 1 : 2 * i; };
   float top = -INFINITY, sum = 0.f;
   f32x16 o[1];
 #pragma unroll
   for (int i = 0; i < 16; ++i) o[0][i] = 0.f;
-  for (int i = w; i <= end; ++i) top = fmaxf(top, f.stats[place(i) * kTile + 32 * wave + c].x);  // (a maximum of NaN is passed over)
-  for (int i = w; i <= end; ++i) {
-    const float2 ml = f.stats[place(i) * kTile + 32 * wave + c];
-    if (ml.x != ml.x) continue;  // the same for all threads
-    const float k = ml.x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml.x - top);
-    sum += ml.y * k;
-    const f32x4* const part = f.parts + (place(i) * (a.c.dim / 8) + 4 * d) * kThreads + threadIdx.x;
+  // two parts are requested at a time, with their maxima
+  for (int i0 = w; i0 <= end; i0 += 2) {
+    float2 ml[2];
+    f32x4 v[2][4];
 #pragma unroll
-    for (int y = 0; y < 4; ++y) {
-      const f32x4 v = part[y * kThreads];
+    for (int k = 0; k < 2; ++k) {
+      const int i = min(i0 + k, end);
+      const int64_t place = i == w ? 2 * i + 1 : 2 * i;
+      ml[k] = f.stats[place * kTile + 32 * wave + c];
+      const f32x4* const part = f.parts + (place * (a.c.dim / 8) + 4 * d) * kThreads + threadIdx.x;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[0][4 * y + e] += v[e] * k;
+      for (int y = 0; y < 4; ++y) v[k][y] = part[y * kThreads];
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const float m = ml[k].x;
+      if (i0 + k > end || m != m) continue;  // (a maximum of NaN: no part; the same for all threads)
+      const float next = fmaxf(top, m), keep = next == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top - next);
+      const float x = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - next);
+      top = next;
+      sum = fmaf(sum, keep, ml[k].y * x);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[0][e] = fmaf(o[0][e], keep, v[k][e / 4][e % 4] * x);
     }
   }
   if (rid >= sp.n * f.group) return;
