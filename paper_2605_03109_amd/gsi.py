@@ -577,9 +577,10 @@ def _rows_of_heads(name: str, t: torch.Tensor, dim: int) -> Tuple[int, int]:
     """(pointer, elements between tokens) of t[T, heads, dim] whose tokens may lie further apart than a row."""
     if not t.is_cuda:
         raise ValueError("libgsi takes device tensors only")
-    if t.dim() != 3 or t.shape[2] != dim or (t.stride(2) != 1 and dim != 1) or (t.stride(1) != dim and t.shape[1] != 1):
-        raise ValueError(f"{name}[T, heads, {dim}] must hold the heads of a token one after another, got {tuple(t.shape)} with strides {t.stride()}")
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1] * dim
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[2] != dim or stride[2] != 1 or (stride[1] != dim and shape[1] != 1):
+        raise ValueError(f"{name}[T, heads, {dim}] must hold the heads of a token one after another, got {tuple(shape)} with strides {stride}")
+    return t.data_ptr(), stride[0] if shape[0] > 1 else shape[1] * dim
 
 
 def kv_tables(kv_len: torch.Tensor, n_new: torch.Tensor, free_pages: torch.Tensor, n_free: torch.Tensor, table: torch.Tensor,
@@ -603,8 +604,9 @@ def kv_tables(kv_len: torch.Tensor, n_new: torch.Tensor, free_pages: torch.Tenso
 
 def kv_append(cache: KvCache, K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor, stream=None) -> None:
     """Rows K, V[T, heads, dim] (fp32 or bf16; tokens may lie further apart than a row) into the cache at slots[T]."""
-    T = K.shape[0]
-    if K.shape != V.shape or K.dtype != V.dtype or K.shape[1] != cache.heads:
+    shape = K.shape
+    T = shape[0]
+    if shape != V.shape or K.dtype != V.dtype or shape[1] != cache.heads:
         raise ValueError(f"K and V[T, {cache.heads}, {cache.dim}] must agree in shape and dtype")
     (kp, ks), (vp, vs) = _rows_of_heads("K", K, cache.dim), _rows_of_heads("V", V, cache.dim)
     _check(lib.gsi_kv_append(ctypes.byref(cache.desc), kp, vp, T, ks, vs, dtype_code(K), _i32("slots", slots, T), _stream(stream)))
@@ -612,13 +614,22 @@ def kv_append(cache: KvCache, K: torch.Tensor, V: torch.Tensor, slots: torch.Ten
 
 def kv_expand(cache: KvCache, slots: torch.Tensor, dtype: torch.dtype = torch.float32, K=None, V=None, stream=None):
     """The values that the cache holds at slots[T]: K, V[T, heads, dim] in `dtype`; zero rows for negative slots."""
-    shape = (slots.numel(), cache.heads, cache.dim)
+    T = slots.numel()
+    shape = (T, cache.heads, cache.dim)
+    given = K is not None or V is not None
     K = _empty(shape, dtype, slots.device, stream) if K is None else K
     V = _empty(shape, dtype, slots.device, stream) if V is None else V
-    if tuple(K.shape) != shape or tuple(V.shape) != shape or K.dtype != V.dtype:
+    if given and (tuple(K.shape) != shape or tuple(V.shape) != shape or K.dtype != V.dtype):
         raise ValueError(f"K and V must be {shape} of one dtype")
-    _check(lib.gsi_kv_expand(ctypes.byref(cache.desc), _i32("slots", slots), slots.numel(), _ptr(K), _ptr(V), dtype_code(K), _stream(stream)))
+    _check(lib.gsi_kv_expand(ctypes.byref(cache.desc), _i32("slots", slots), T, _ptr(K), _ptr(V), dtype_code(K), _stream(stream)))
     return K, V
+
+
+@functools.lru_cache(maxsize=4096, typed=True)  # (of the sizes alone, as workspace_bytes)
+def _kv_workspace_bytes(n_pages: int, kv_heads: int, dim: int, page: int, T: int, heads: int, dt: int, B: int, max_q: int, max_len: int) -> int:
+    somewhere = 256  # (the query asks for buffers and reads none)
+    desc = KvCacheDesc(somewhere, somewhere, somewhere, somewhere, n_pages, kv_heads, dim, page, 0)
+    return int(lib.gsi_kv_attention_workspace_bytes(ctypes.byref(desc), T, heads, dt, B, max_q, max_len))
 
 
 def kv_attention(cache: KvCache, Q: torch.Tensor, q_start: Optional[torch.Tensor], kv_len: torch.Tensor, table: torch.Tensor,
@@ -631,27 +642,30 @@ def kv_attention(cache: KvCache, Q: torch.Tensor, q_start: Optional[torch.Tensor
     B = kv_len.numel()
     if dim != cache.dim:
         raise ValueError(f"Q has heads of {dim} elements, the cache of {cache.dim}")
-    if table.dim() != 2 or table.shape[0] != B:
-        raise ValueError(f"table must be [{B}, width], got {tuple(table.shape)}")
+    rows = table.shape
+    if len(rows) != 2 or rows[0] != B:
+        raise ValueError(f"table must be [{B}, width], got {tuple(rows)}")
+    width = rows[1]
     qp, qs = _rows_of_heads("Q", Q, dim)
-    O = _empty((T, heads, dim), Q.dtype, Q.device, stream) if O is None else O
-    if tuple(O.shape) != (T, heads, dim) or O.dtype != Q.dtype:
+    if O is None:
+        O = _empty((T, heads, dim), Q.dtype, Q.device, stream)
+    elif tuple(O.shape) != (T, heads, dim) or O.dtype != Q.dtype:
         raise ValueError("O must have Q's shape and dtype")
     if lse is True:
         lse = _empty((T, heads), torch.float32, Q.device, stream)
     elif lse is False:
         lse = None
-    if lse is not None and (tuple(lse.shape) != (T, heads) or lse.dtype != torch.float32):
+    elif lse is not None and (tuple(lse.shape) != (T, heads) or lse.dtype != torch.float32):
         raise ValueError("lse must be fp32 [T, heads]")
     if max_q is None:
         max_q = 1 if q_start is None else max(T, 1)
     if max_len is None:
-        max_len = table.shape[1] * cache.page
+        max_len = width * cache.page
     dt, desc = dtype_code(Q), ctypes.byref(cache.desc)
     max_q, max_len = max(int(max_q), 1), max(int(max_len), 1)
-    need = int(lib.gsi_kv_attention_workspace_bytes(desc, T, heads, dt, B, max_q, max_len))
+    need = _kv_workspace_bytes(cache.desc.n_pages, cache.heads, dim, cache.page, T, heads, dt, B, max_q, max_len)
     wsp, wsn, held = _ws_args(ws, need, stream)
     _check(lib.gsi_kv_attention(desc, qp, T, heads, qs, dt, None if q_start is None else _i32("q_start", q_start, B + 1),
-                                _i32("kv_len", kv_len), B, _i32("table", table), table.shape[1], max_q, max_len,
+                                _i32("kv_len", kv_len), B, _i32("table", table), width, max_q, max_len,
                                 dim ** -0.5 if scale is None else float(scale), _ptr(O), _ptr(lse), wsp, wsn, _stream(stream)))
     return O if lse is None else (O, lse)
