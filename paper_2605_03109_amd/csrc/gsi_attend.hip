@@ -847,12 +847,13 @@ hipError_t attend_few(const KvAttend& a, int64_t few, void* ws, hipStream_t s) {
 // Which kernels a call takes, by the rows that its longest request has to a head of keys (tokens times heads that share it).  The workgroups of few rows
 // read the keys once for 16 rows, those of many rows once for 128 but with a step that costs them as much for 20 rows as for 128.
 // us a call, few / many rows, 8 heads of keys:
-//   up to 16 rows: few.  16 rows, 16 requests of up to 4000 keys x 128: bf16 35 / 47, fp32 41 / 75.
+//   up to 16 rows: few.  16 rows, 16 requests of up to 4000 keys x 128: bf16 34 / 46, fp32 42 / 78.
 //   up to 32: few, but for bf16 over short contexts of many requests, where few rows are cut and joined and many are not.  32 rows, 64 requests of up to
-//     4000 keys: x 64 62 / 77, x 128 76 / 82, x 256 169 / 238, fp32 x 128 106 / 200; of up to 700: bf16 x 128 47 / 27.
-//   up to 64: few where that makes a tile for each workgroup at most (64 rows, 8 requests of up to 4000: bf16 40 / 45, fp32 50 / 77), and for fp32 rows of 128
-//     and more, whose products are three (64 requests: x 128 174 / 218, x 256 699 / 1094; x 64 124 / 108).
-//   more: many (128 rows, 64 requests of up to 700: bf16 80 / 37, fp32 110 / 76).
+//     4000 keys: x 64 60 / 77, x 128 75 / 80, x 256 128 / 235, fp32 x 128 105 / 215; of up to 700: bf16 x 128 47 / 26.
+//   up to 64: few where that makes a tile for each workgroup at most (64 rows, 8 requests of up to 4000 keys x 128: bf16 39 / 44, fp32 51 / 79), and for fp32
+//     rows of 128 and more, whose products are three, and the widest heads (64 requests: fp32 x 128 170 / 231, x 256 322 / 505; bf16 x 256 213 /
+//     245; not so x 128 113 / 91, fp32 x 64 123 / 106).
+//   more: many (128 rows, 64 requests of up to 700: bf16 78 / 36, fp32 111 / 79; fp32 x 256 of up to 4000 589 / 589).
 // A call of single tokens and prompts takes both kernels, each for its requests, where the mean request has few rows.  both / many rows: 63 single tokens
 // behind 100 to 4000 keys and a prompt of 128, 32 heads of keys, bf16 120 / 192, fp32 191 / 492; requests of 1 to 64 tokens, four heads to
 // one of keys (60 rows in the mean), bf16 87 / 61.
