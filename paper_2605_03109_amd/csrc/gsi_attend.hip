@@ -855,9 +855,12 @@ hipError_t attend_few(const KvAttend& a, int64_t few, void* ws, hipStream_t s) {
 //     245; not so x 128 113 / 91, fp32 x 64 123 / 106).
 //   more: many (128 rows, 64 requests of up to 700: bf16 78 / 36, fp32 111 / 79; fp32 x 256 of up to 4000 589 / 589).
 // A call of single tokens and prompts takes both kernels, each for its requests, where the mean request has few rows.  both / many rows: 63 single tokens
-// behind 100 to 4000 keys and a prompt of 128, 32 heads of keys, bf16 120 / 192, fp32 191 / 492; requests of 1 to 64 tokens, four heads to
-// one of keys (60 rows in the mean), bf16 87 / 61.
-constexpr int64_t kFewRows = 16, kBothRows = 32;
+// behind 100 to 4000 keys and a prompt of 128, 32 heads of keys, bf16 115 / 192, fp32 166 / 492; requests of 1 to 64 tokens, four heads to
+// one of keys (60 rows in the mean), bf16 87 / 61.  The few are then single tokens and others of up to 8 rows, whose tiles are small.  us with 8 / with
+// 32 rows (tiles of 16): 250 single tokens and a prompt of 1024, 32 heads of keys, bf16 205 / 212, fp32 260 / 307, 8 heads of keys fp32 145 /
+// 163; 60 requests of 3 tokens and a prompt of 512, 32 heads of keys, fp32 156 / 177, but 8 heads of keys (12 rows) 158 / 130.
+constexpr int64_t kFewRows = 16;
+static int64_t both_rows(const KvAttend& a) { return std::max(a.heads / a.c.heads, 8); }
 enum Kernels { kFewOnly, kPromptOnly, kBoth };
 static Kernels kernels_of(const KvAttend& a) {
   const int64_t group = a.heads / a.c.heads, rows = std::min(a.max_q, a.T) * group;
@@ -872,7 +875,7 @@ size_t kv_attention_workspace(const KvAttend& a) {
   switch (kernels_of(a)) {
     case kFewOnly: return attend_few_workspace(a, INT64_MAX);
     case kPromptOnly: return attend_prompt_workspace(a);
-    default: return attend_few_workspace(a, kBothRows) + attend_prompt_workspace(a);
+    default: return attend_few_workspace(a, both_rows(a)) + attend_prompt_workspace(a);
   }
 }
 
@@ -882,8 +885,8 @@ hipError_t kv_attention(const KvAttend& a, void* ws, hipStream_t s) {
     case kPromptOnly: return attend_prompt(a, 0, true, ws, s);
     default: break;
   }
-  if (hipError_t e = attend_few(a, kBothRows, ws, s); e != hipSuccess) return e;
-  return attend_prompt(a, kBothRows, false, static_cast<char*>(ws) + attend_few_workspace(a, kBothRows), s);
+  if (hipError_t e = attend_few(a, both_rows(a), ws, s); e != hipSuccess) return e;
+  return attend_prompt(a, both_rows(a), false, static_cast<char*>(ws) + attend_few_workspace(a, both_rows(a)), s);
 }
 
 }  // namespace gsi
