@@ -169,8 +169,8 @@ __device__ __forceinline__ void load_values(Values<DPL>& v, const KvAttend& a, c
 // query, of a weight) are rows of one product instead of three products: row r's terms are the registers of lane group r of the scores,
 // which are added, and the registers of lane groups 2 r and 2 r + 1 (even, odd elements) of the output, which are added at the end.  TWO: four rows of
 // bf16, whose weights have a second term in the rows of the second product that would be idle: the output is then off by its own rounding alone
-// (to 64 bits 0.0017 of it; with one term 0.0024).  More rows of bf16 have one term: a second takes products of its own (8 rows x 256 51 us, so 49; 16
-// rows x 128 84, so 75).
+// (to 64 bits 0.0017 of it; with one term 0.0024).  More rows of bf16 have one term: a second takes products of its own (8 rows x 256 51 us, with one 49; 16
+// rows x 128 84, with one 75).
 template <bool F, int NR>
 struct Rows {
   static constexpr bool kFold = F && NR == 0;
