@@ -32,15 +32,21 @@ constexpr float kSlack = 8.f;
 __device__ __forceinline__ float exponent_scale(float scale) { return fmaxf(fabsf(scale) * kLog2e, 1.17549435e-38f); }
 
 struct Span {  // a request's tokens of the call and its keys
-  int t0, n, len;
+  int t0, n;
+  int len;   // keys that its row of the table has places for
+  int past;  // keys in front of its first token of the call, whether there are places for them or not (below 0: so many tokens see none)
+  // the last key that token i sees
+  __device__ __forceinline__ int last_key(int i) const { return min(past + i, len - 1); }
 };
+__device__ __forceinline__ int places(const KvAttend& a, const Span& s) { return (int)min((int64_t)s.past + s.n, a.width << a.c.page_shift); }
 __device__ __forceinline__ Span span_of(const KvAttend& a, int b) {
   Span s;
   const int T = (int)a.T;
   s.t0 = a.q_start ? min(max(a.q_start[b], 0), T) : min(b, T);
   const int t1 = a.q_start ? min(max(a.q_start[b + 1], s.t0), T) : min(b + 1, T);
   s.n = t1 - s.t0;
-  s.len = (int)min((int64_t)max(a.kv_len[b], 0), a.width << a.c.page_shift);
+  s.past = max(a.kv_len[b], 0) - s.n;
+  s.len = places(a, s);
   return s;
 }
 
@@ -68,14 +74,14 @@ constexpr int kScan = 256;
 struct Prefix {
   int64_t incl[kScan];
   int64_t sums[kScan / kWave];
-  Span span[kScan];
+  int t0[kScan], n[kScan], past[kScan];
 };
 template <class U>
 __device__ __forceinline__ int64_t scan_requests(const KvAttend& a, int64_t b0, Prefix& x, U units) {
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const int64_t b = b0 + threadIdx.x;
   int64_t v = 0;
-  Span sp{0, 0, 0};
+  Span sp{0, 0, 0, 0};
   if (b < a.B) {
     sp = span_of(a, (int)b);
     v = units(sp);
@@ -96,7 +102,9 @@ __device__ __forceinline__ int64_t scan_requests(const KvAttend& a, int64_t b0, 
     total += x.sums[w];
   }
   x.incl[threadIdx.x] = v;
-  x.span[threadIdx.x] = sp;
+  x.t0[threadIdx.x] = sp.t0;
+  x.n[threadIdx.x] = sp.n;
+  x.past[threadIdx.x] = sp.past;
   __syncthreads();
   return total;
 }
@@ -107,7 +115,12 @@ __device__ __forceinline__ int64_t total_units(const KvAttend& a, Prefix& x, U u
   return total;
 }
 // (the first 256 requests' spans stay in LDS unless there are more requests)
-__device__ __forceinline__ Span span_at(const KvAttend& a, const Prefix& x, int b) { return a.B <= kScan ? x.span[b] : span_of(a, b); }
+__device__ __forceinline__ Span span_at(const KvAttend& a, const Prefix& x, int b) {
+  if (a.B > kScan) return span_of(a, b);
+  Span s{x.t0[b], x.n[b], 0, x.past[b]};
+  s.len = places(a, s);
+  return s;
+}
 
 // The request of unit u (a wave's own) after total_units, and the units before it; the first one where u is past the end.
 struct Place {

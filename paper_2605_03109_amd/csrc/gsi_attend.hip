@@ -282,6 +282,7 @@ __global__ __launch_bounds__(kThreads, few_resident(sizeof(typename X::storage) 
     sp.t0 = __builtin_amdgcn_readfirstlane(sp.t0);
     sp.n = __builtin_amdgcn_readfirstlane(sp.n);
     sp.len = __builtin_amdgcn_readfirstlane(sp.len);
+    sp.past = __builtin_amdgcn_readfirstlane(sp.past);
     const int seg = __builtin_amdgcn_readfirstlane(f.whole ? (int)(u - before) : (int)divide(u - before, per));
     const int64_t seg_begin = before + (int64_t)seg * per;
     const int tile = f.by_heads(seg), kvh = seg - tile * a.c.heads;
@@ -347,13 +348,13 @@ __global__ __launch_bounds__(kThreads, few_resident(sizeof(typename X::storage) 
     }
     // the last key that a row sees: by the layout of the scores, and of the output (the same but where terms are folded)
     int lim[NS], lim_o[NS];
-    const auto last_key = [&](int r) { return r < rows ? sp.len - sp.n + f.by_group(tile * TR + r) : -1; };
+    const auto last_key = [&](int r) { return r < rows ? sp.last_key(f.by_group(tile * TR + r)) : -1; };
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
       lim[i] = last_key(L.g + 4 * i);
       lim_o[i] = R::kFold ? last_key(L.g / 2) : lim[i];
     }
-    const int lim_low = sp.len - sp.n + f.by_group(tile * TR);  // what every row of the tile sees
+    const int lim_low = sp.last_key(f.by_group(tile * TR));  // what every row of the tile sees
 
     f32x4 o[NO][JP];
     float m[NS], l[NS];

