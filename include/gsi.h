@@ -345,8 +345,11 @@ typedef struct gsi_kv_cache {
  * free_cap entries are there), in the order of the requests, and entered in table[B, width]; entries that are there stay.
  *   kv_len_out[b] = kv_len[b] + n_new[b];  q_start[0 .. B]: first token of each request among the step's tokens;
  *   slots[t], positions[t] of the step's tokens t < q_start[B], -1 for the rest of T;
- *   status[0] = pages taken, status[1] = pages that were wanted and not there (none free, or the table too narrow): their
- *   entries and their tokens' slots are -1.
+ *   status[0] = pages taken, status[1] = pages that the step's tokens lie on and that are not there (none free now or in the step
+ *   that began the page, or the table too narrow): their entries and their tokens' slots are -1.  0: every token has a slot.
+ * kv_len_out counts the tokens without a slot too.  Called again from the same kv_len once pages came back, the step loses nothing; from kv_len_out
+ * on those tokens are lost, and with them what the request has later on the page that it had begun without one (such an entry is not
+ * filled: the page would hold another request's rows in the places of the lost ones).
  * Negative lengths count as 0, lengths above 2^30 as that many; T is at most 2^29.  Where the step has more than T tokens,
  * the last are dropped from the requests' n_new.  B = 0: nothing is written.
  * kv_len, n_new and free_pages are not changed: the caller's free list begins status[0] entries later.  No output may lie over an

@@ -71,6 +71,7 @@ __global__ __launch_bounds__(kScanThreads) void tables_kernel(const int32_t* __r
   const auto len_of = [&](int b) { return min(max(kv_len[b], 0), kMost); };
   const auto pages = [&](int len) { return (len + page - 1) >> page_shift; };  // len <= 2^31 - 4096
   const auto held = [&](int n) { return (int)min((int64_t)n, width); };
+  const auto names_page = [&](int entry) { return entry >= 0 && entry <= (0x7fffffff >> page_shift); };  // one whose slots are numbers
   int carry = 0;
   for (int b0 = 0; b0 < B; b0 += kScanThreads) {
     const int b = b0 + threadIdx.x;
@@ -87,6 +88,8 @@ __global__ __launch_bounds__(kScanThreads) void tables_kernel(const int32_t* __r
       const int len = len_of(b), have = pages(len), need = pages(len + (tok[b + 1] - tok[b]));
       all = need - have;
       in_table = held(need) - held(have);
+      // new tokens on a page that was begun before: it may be one that was not there then (the entries of this call lie behind it)
+      if (blockIdx.x == 0 && tok[b + 1] > tok[b] && (len & (page - 1)) && !(have <= width && names_page(table[b * width + have - 1]))) ++all;
     }
     const int at = block_scan(in_table, kMost, carry_pages, wave_sums);
     block_scan(all, kMost, carry_all, wave_sums);
@@ -118,7 +121,7 @@ __global__ __launch_bounds__(kScanThreads) void tables_kernel(const int32_t* __r
       const int j = pos >> page_shift;
       // entries of this call are not read back: another workgroup may not have written them yet
       const int entry = j >= width ? -1 : (j < have ? table[b * width + j] : fresh(first[b] + j - have));
-      if (entry >= 0 && entry <= (0x7fffffff >> page_shift)) slot = (entry << page_shift) + (pos & (page - 1));
+      if (names_page(entry)) slot = (entry << page_shift) + (pos & (page - 1));
     }
     slots[t] = slot;
     positions[t] = pos;
