@@ -20,7 +20,9 @@ from paper_2605_03109_amd import gsi
 
 class AttentionBlock:
     """Weights W[m, d] and bases U[d, k] (one for the input of q, k, v, one for that of o), a cache of `n_pages` pages for up
-    to `requests` requests of up to `max_len` tokens."""
+    to `requests` requests of up to `max_len` tokens.  Requests keep their pages; tokens behind the last page or past `max_len` have no place in
+    the cache, and `missing` says so: it is the number of pages that were not there, summed over the steps (on the device, 0 where nothing was lost;
+    a step whose `status[1]` is not 0 has lost tokens, and its requests are to be dropped or given again)."""
 
     def __init__(self, weights: Dict[str, torch.Tensor], U_in: torch.Tensor, U_out: torch.Tensor, heads: int, kv_heads: int,
                  requests: int, n_pages: int, max_len: int, page: int = 64, eps: float = 0.05):
@@ -35,9 +37,19 @@ class AttentionBlock:
         self.table = torch.full((requests, -(-max_len // page)), -1, **i32)
         self.kv_len = torch.zeros(requests, **i32)
         self.free = torch.arange(n_pages, **i32)
-        self.n_free = torch.full((1,), n_pages, **i32)
+        self._count = torch.tensor([n_pages, 0], **i32)  # free pages, missing ones
+        self._change = torch.tensor([-1, 1], **i32)      # of them, by the tables' status
+        self.status = torch.zeros(2, **i32)              # of the last step: pages taken, pages that were not there
         self._place = torch.arange(n_pages, device=dev)
         self._stacks: Dict[int, tuple] = {}
+
+    @property
+    def n_free(self) -> torch.Tensor:
+        return self._count[:1]
+
+    @property
+    def missing(self) -> torch.Tensor:
+        return self._count[1:]
 
     def _stacks_for(self, T: int) -> tuple:
         if T not in self._stacks:
@@ -57,10 +69,10 @@ class AttentionBlock:
         T = X.shape[0]
         x, attended, qkv, out = self._stacks_for(T)
         x.copy_(X)
-        self.kv_len, start, slots, _, status = gsi.kv_tables(self.kv_len, n_new, self.free, self.n_free, self.table, T, self.cache.page)
+        self.kv_len, start, slots, _, self.status = gsi.kv_tables(self.kv_len, n_new, self.free, self.n_free, self.table, T, self.cache.page)
         # what was taken leaves the front of the free list
-        self.free = self.free[(self._place + status[0]).clamp(max=self.free.numel() - 1)]
-        self.n_free = self.n_free - status[:1]
+        self.free = self.free[(self._place + self.status[0]).clamp(max=self.free.numel() - 1)]
+        self._count = torch.addcmul(self._count, self.status, self._change)
         qkv.run()
         q, k, v = (m["Y"].view(T, -1, self.dim) for m in qkv.maps_t)
         gsi.kv_append(self.cache, k, v, slots)
@@ -107,12 +119,15 @@ def main() -> int:
         for _ in range(args.steps):
             block.step(tokens, one, 1)
 
-    state = block.kv_len, block.free, block.n_free
+    state = block.kv_len, block.free, block._count
     block.step(prompt, n_new, args.prompt), block.step(tokens, one, 1)  # first calls
-    block.kv_len, block.free, block.n_free = state
+    block.kv_len, block.free, block._count = state
     block.table.fill_(-1)
     prompt_s = timed(lambda: block.step(prompt, n_new, args.prompt))
     decode_s = timed(decode)
+    if int(block.missing):
+        print("serve.py: the cache had too few pages, tokens were lost", file=sys.stderr)
+        return 1
     print(json.dumps({"workload": f"attention half of a block, d {d}, {args.heads} heads over {args.kv_heads}, rank {args.k}, {args.requests} requests",
                       "prompt_tokens": sum(lens), "prompt_ms": round(prompt_s * 1e3, 3), "decode_steps": args.steps,
                       "decode_us_per_step": round(decode_s / args.steps * 1e6, 1),
