@@ -8,6 +8,7 @@ shapes of an OPT-6.7B layer by default) and prints one JSON line with the times 
 from __future__ import annotations
 
 import argparse
+import collections
 import json
 import sys
 import time
@@ -41,7 +42,7 @@ class AttentionBlock:
         self._change = torch.tensor([-1, 1], **i32)      # of them, by the tables' status
         self.status = torch.zeros(2, **i32)              # of the last step: pages taken, pages that were not there
         self._place = torch.arange(n_pages, device=dev)
-        self._stacks: Dict[int, tuple] = {}
+        self._stacks: collections.OrderedDict[tuple, tuple] = collections.OrderedDict()
 
     @property
     def n_free(self) -> torch.Tensor:
@@ -51,8 +52,16 @@ class AttentionBlock:
     def missing(self) -> torch.Tensor:
         return self._count[1:]
 
+    KEPT = 8  # step sizes whose buffers are kept, in order of use
+
     def _stacks_for(self, T: int) -> tuple:
-        if T not in self._stacks:
+        # buffers by stream too: memory that one gives back is used again behind the work of its own stream only
+        key = T, torch.cuda.current_stream(self.U_in.device).cuda_stream
+        if key in self._stacks:
+            self._stacks.move_to_end(key)
+        else:
+            while len(self._stacks) >= self.KEPT:
+                self._stacks.popitem(last=False)
             f32 = dict(dtype=torch.float32, device=self.U_in.device)
             X = torch.empty((T, self.U_in.shape[0]), **f32)
             A = torch.empty((T, self.heads, self.dim), **f32)
@@ -60,12 +69,13 @@ class AttentionBlock:
                                  [{"W": self.W[n], "M": self.M[n], "input_id": 0} for n in "qkv"], T, self.eps)
             out = gsi.LayerStack([{"U": self.U_out, "X": A.view(T, -1)}], [{"W": self.W["o"], "M": self.M["o"], "input_id": 0}],
                                  T, self.eps)
-            self._stacks[T] = (X, A, qkv, out)
-        return self._stacks[T]
+            self._stacks[key] = (X, A, qkv, out)
+        return self._stacks[key]
 
     def step(self, X: torch.Tensor, n_new: torch.Tensor, max_q: int, max_len: Optional[int] = None) -> torch.Tensor:
         """X[T, d] (fp32): the step's tokens, request by request; n_new[requests] int32: how many each has; max_q, max_len: the most
-        that one has, new and altogether.  Returns the output of map o, [T, d] (valid until the next step of T tokens)."""
+        that one has, new and altogether.  Returns the output of map o, [T, d] (valid until the next step of T tokens; a step of a size that is
+        not among the last KEPT sets its buffers up first)."""
         T = X.shape[0]
         x, attended, qkv, out = self._stacks_for(T)
         x.copy_(X)
