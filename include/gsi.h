@@ -353,18 +353,19 @@ typedef struct gsi_kv_cache {
  * Negative lengths count as 0, lengths above 2^30 as that many; T is at most 2^29.  Where the step has more than T tokens,
  * the last are dropped from the requests' n_new.  B = 0: nothing is written.
  * kv_len, n_new and free_pages are not changed: the caller's free list begins status[0] entries later.  No output may lie over an
- * input (refused).  The same call again gives the same results (the table's new entries are written again). */
+ * input or another output (refused).  The same call again gives the same results (the table's new entries are written again). */
 int gsi_kv_tables(const int32_t* kv_len, const int32_t* n_new, int64_t B, const int32_t* free_pages, const int32_t* n_free,
                   int64_t free_cap, int32_t* table, int64_t width, int64_t page, int64_t T, int32_t* kv_len_out, int32_t* q_start,
                   int32_t* slots, int32_t* positions, int32_t* status, void* stream);
 
 /* Rows of T tokens into the cache: K and V in `dtype`, token t at K + t * k_stride elements, its heads one after another
- * [heads, dim]; slots[t] as above, a slot that is negative or past the cache's end is skipped.  No slot may come twice. */
+ * [heads, dim]; slots[t] as above, a slot that is negative or past the cache's end is skipped.  No slot may come twice, and no
+ * input may lie in the cache (refused). */
 int gsi_kv_append(const gsi_kv_cache* cache, const void* K, const void* V, int64_t T, int64_t k_stride, int64_t v_stride, int dtype,
                   const int32_t* slots, void* stream);
 
 /* The reverse: the values that the cache holds at slots[t], as K[T, heads, dim] and V in `dtype` (exact in both), 16-byte
- * aligned.  Rows whose slot is negative or past the cache's end are zero. */
+ * aligned.  Rows whose slot is negative or past the cache's end are zero.  Neither output may lie over the other or an input (refused). */
 int gsi_kv_expand(const gsi_kv_cache* cache, const int32_t* slots, int64_t T, void* K, void* V, int dtype, void* stream);
 
 /* Attention of the step's T tokens over their requests' keys, the step's own included: kv_len[b] keys in the pages of
@@ -378,6 +379,7 @@ int gsi_kv_expand(const gsi_kv_cache* cache, const int32_t* slots, int64_t T, vo
  * numbers cost time and never change what is computed.
  * Arithmetic: fp32 sums and statistics of bf16 products; keys and values are exact in bf16, queries and weights exp(s - max) enter in
  * one bf16 term (bf16: a query itself, a weight rounded once; for up to four rows in two terms) or in three (fp32).
+ * O may be Q itself (the same address, q_stride of a row); else O, lse and ws lie apart from each other and the inputs (refused).
  * ws: gsi_kv_attention_workspace_bytes(). */
 int gsi_kv_attention(const gsi_kv_cache* cache, const void* Q, int64_t T, int64_t heads, int64_t q_stride, int dtype,
                      const int32_t* q_start, const int32_t* kv_len, int64_t B, const int32_t* table, int64_t width, int64_t max_q,

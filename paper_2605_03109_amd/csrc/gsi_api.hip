@@ -81,6 +81,33 @@ int check_ws_level(const char* fn, const void* ws, size_t ws_bytes, Bytes bytes,
   return check_ws(fn, ws, ws_bytes, bytes(kWsFirst));
 }
 
+// ---- what the calls of the 4-bit cache read and write: outputs over inputs are refused -----------------------
+struct Bytes {  // what a call reads or writes
+  const void* p;
+  uint64_t n;  // 0: nothing
+};
+bool overlap(const Bytes& x, const Bytes& y) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(x.p), b = reinterpret_cast<uintptr_t>(y.p);
+  return x.n > 0 && y.n > 0 && a < b + y.n && b < a + x.n;
+}
+// Workgroups read inputs while others write outputs.
+template <size_t I, size_t O>
+int check_apart(const char* fn, const Bytes (&in)[I], const Bytes (&out)[O]) {
+  for (size_t i = 0; i < O; ++i) {
+    for (const Bytes& x : in)
+      if (overlap(x, out[i])) return fail(GSI_ERR_SHAPE, "%s: an output lies over an input", fn);
+    for (size_t j = i + 1; j < O; ++j)
+      if (overlap(out[i], out[j])) return fail(GSI_ERR_SHAPE, "%s: an output lies over another", fn);
+  }
+  return GSI_OK;
+}
+Bytes codes_of(const gsi::KvView& c, const uint8_t* p) { return {p, (uint64_t)c.code_at(c.n_pages, 0)}; }
+Bytes scales_of(const gsi::KvView& c, const uint8_t* p) { return {p, (uint64_t)c.scale_at(c.n_pages, 0)}; }
+Bytes rows_of(const void* p, int64_t T, int64_t stride, int64_t row, int dtype) {  // (as far as addresses go)
+  const unsigned __int128 n = ((unsigned __int128)(T - 1) * (uint64_t)(T > 1 ? stride : 0) + (uint64_t)row) * gsi::elem_size(dtype);
+  return {p, (uint64_t)std::min<unsigned __int128>(n, UINTPTR_MAX - reinterpret_cast<uintptr_t>(p))};
+}
+
 }  // namespace
 
 extern "C" {
@@ -1939,18 +1966,14 @@ int gsi_kv_tables(const int32_t* kv_len, const int32_t* n_new, int64_t B, const 
   if (T > 0) GSI_REQUIRE_PTR(slots);
   if (T > 0) GSI_REQUIRE_PTR(positions);
   GSI_REQUIRE_PTR(status);
-  const struct { const void* p; int64_t n; } in[] = {{kv_len, B}, {n_new, B}, {free_pages, free_cap}, {n_free, 1}},
-                                             out[] = {{table, B * width}, {kv_len_out, B}, {q_start, B + 1}, {slots, T}, {positions, T}, {status, 2}};
-  for (const auto& x : in)
+  const Bytes in[] = {{kv_len, 4 * (uint64_t)B}, {n_new, 4 * (uint64_t)B}, {free_pages, 4 * (uint64_t)free_cap}, {n_free, 4}},
+              out[] = {{table, 4 * (uint64_t)(B * width)}, {kv_len_out, 4 * (uint64_t)B}, {q_start, 4 * (uint64_t)(B + 1)},
+                       {slots, 4 * (uint64_t)T}, {positions, 4 * (uint64_t)T}, {status, 8}};
+  for (const Bytes& x : in)
     if (!aligned(x.p, 4)) return fail(GSI_ERR_ALIGN, "%s: a pointer is not 4-byte aligned", fn);
-  for (const auto& y : out) {
+  for (const Bytes& y : out)
     if (!aligned(y.p, 4)) return fail(GSI_ERR_ALIGN, "%s: a pointer is not 4-byte aligned", fn);
-    for (const auto& x : in) {
-      const uintptr_t a = reinterpret_cast<uintptr_t>(x.p), b = reinterpret_cast<uintptr_t>(y.p);
-      if (x.n > 0 && y.n > 0 && a < b + 4 * (uintptr_t)y.n && b < a + 4 * (uintptr_t)x.n)
-        return fail(GSI_ERR_SHAPE, "%s: an output lies over an input: workgroups read the inputs while others write", fn);
-    }
-  }
+  if (int rc = check_apart(fn, in, out)) return rc;
   hipError_t e = gsi::kv_tables(kv_len, n_new, B, free_pages, n_free, free_cap, table, width, __builtin_ctzll((unsigned long long)page), T,
                                 kv_len_out, q_start, slots, positions, status, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? GSI_OK : hip_fail(e, fn);
@@ -1973,6 +1996,10 @@ int gsi_kv_append(const gsi_kv_cache* cache, const void* K, const void* V, int64
   GSI_REQUIRE_ALIGNED(K, gsi::elem_size(dtype));
   GSI_REQUIRE_ALIGNED(V, gsi::elem_size(dtype));
   GSI_REQUIRE_ALIGNED(slots, 4);
+  // (keys and values of a cache may share buffers)
+  const Bytes in[] = {rows_of(K, T, k_stride, row, dtype), rows_of(V, T, v_stride, row, dtype), {slots, 4 * (uint64_t)T}};
+  for (const Bytes& y : {codes_of(c, c.K), scales_of(c, c.Ks), codes_of(c, c.V), scales_of(c, c.Vs)})
+    if (int rc = check_apart(fn, in, {y})) return rc;
   hipError_t e = gsi::kv_append(c, K, V, T, k_stride, v_stride, dtype, slots, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? GSI_OK : hip_fail(e, fn);
 }
@@ -1990,6 +2017,10 @@ int gsi_kv_expand(const gsi_kv_cache* cache, const int32_t* slots, int64_t T, vo
   GSI_REQUIRE_ALIGNED(K, 16);
   GSI_REQUIRE_ALIGNED(V, 16);
   GSI_REQUIRE_ALIGNED(slots, 4);
+  const int64_t row = (int64_t)c.heads * c.dim;
+  const Bytes in[] = {codes_of(c, c.K), scales_of(c, c.Ks), codes_of(c, c.V), scales_of(c, c.Vs), {slots, 4 * (uint64_t)T}},
+              out[] = {rows_of(K, T, row, row, dtype), rows_of(V, T, row, row, dtype)};
+  if (int rc = check_apart(fn, in, out)) return rc;
   hipError_t e = gsi::kv_expand(c, slots, T, K, V, dtype, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? GSI_OK : hip_fail(e, fn);
 }
@@ -2044,7 +2075,16 @@ int gsi_kv_attention(const gsi_kv_cache* cache, const void* Q, int64_t T, int64_
   a.scale = scale;
   a.O = O;
   a.lse = lse;
-  if (int rc = check_ws(fn, ws, ws_bytes, gsi::kv_attention_workspace(a))) return rc;
+  const size_t need = gsi::kv_attention_workspace(a);
+  if (int rc = check_ws(fn, ws, ws_bytes, need)) return rc;
+  // O may be Q itself, row for row: whoever stores a row is the last to read it
+  const int64_t row = heads * a.c.dim;
+  const bool in_place = O == Q && (T == 1 || q_stride == row);
+  const Bytes in[] = {in_place ? Bytes{Q, 0} : rows_of(Q, T, q_stride, row, dtype), {q_start, q_start ? 4 * (uint64_t)(B + 1) : 0},
+                      {kv_len, 4 * (uint64_t)B}, {table, 4 * (uint64_t)(B * width)},
+                      codes_of(a.c, a.c.K), scales_of(a.c, a.c.Ks), codes_of(a.c, a.c.V), scales_of(a.c, a.c.Vs)},
+              out[] = {rows_of(O, T, row, row, dtype), {lse, lse ? 4 * (uint64_t)(T * heads) : 0}, {ws, need}};
+  if (int rc = check_apart(fn, in, out)) return rc;
   hipError_t e = gsi::kv_attention(a, ws, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? GSI_OK : hip_fail(e, fn);
 }
