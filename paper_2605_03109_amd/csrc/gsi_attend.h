@@ -224,13 +224,19 @@ __device__ __forceinline__ float row16_sum(float v) {
 // Rows of tokens that belong to no request: zero.
 template <class X>
 __device__ __forceinline__ void clear_idle_rows(const KvAttend& a) {
-  const int64_t t0 = !a.q_start ? a.T : a.B > 0 ? min(max(a.q_start[a.B], 0), (int)a.T) : 0;
+  if (!a.q_start) return;
+  // in front of the first request's, and behind the last one's
+  const int64_t first = a.B > 0 ? min(max(a.q_start[0], 0), (int)a.T) : 0;
+  const int64_t t0 = a.B > 0 ? min(max(a.q_start[a.B], (int)first), (int)a.T) : 0;
   typename X::storage* const O = reinterpret_cast<typename X::storage*>(a.O);
   const int64_t row = (int64_t)a.heads * a.c.dim, all = (int64_t)gridDim.x * gridDim.y * blockDim.x;
   const int64_t me = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * blockDim.x + threadIdx.x;
   for (int64_t i = t0 * row + me; i < a.T * row; i += all) X::store(O, i, 0.f);
-  if (a.lse)
+  for (int64_t i = me; i < first * row; i += all) X::store(O, i, 0.f);
+  if (a.lse) {
     for (int64_t i = t0 * a.heads + me; i < a.T * a.heads; i += all) a.lse[i] = -INFINITY;
+    for (int64_t i = me; i < first * a.heads; i += all) a.lse[i] = -INFINITY;
+  }
 }
 
 // A rare path that is to stay a branch: the compiler would compute both sides for every element.  The condition is the same in every lane.
