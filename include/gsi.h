@@ -378,7 +378,8 @@ int gsi_kv_expand(const gsi_kv_cache* cache, const int32_t* slots, int64_t T, vo
  * max_q, max_len: the most new tokens and keys that a request is expected to have.  They choose kernels and their launches; other
  * numbers cost time and never change what is computed.
  * Arithmetic: fp32 sums and statistics of bf16 products; keys and values are exact in bf16, queries and weights exp(s - max) enter in
- * one bf16 term (bf16: a query itself, a weight rounded once; for up to four rows in two terms) or in three (fp32).
+ * one bf16 term (bf16: a query itself, a weight rounded once; for up to four rows in two terms) or in three (fp32; what a query has below
+ * 2^-133 is lost, which counts where scale is 2^90 and more).  |scale| < 2.3e38: scale * log2(e) is a number too.
  * O may be Q itself (the same address, q_stride of a row); else O, lse and ws lie apart from each other and the inputs (refused).
  * ws: gsi_kv_attention_workspace_bytes(). */
 int gsi_kv_attention(const gsi_kv_cache* cache, const void* Q, int64_t T, int64_t heads, int64_t q_stride, int dtype,

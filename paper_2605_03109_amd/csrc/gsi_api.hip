@@ -2059,7 +2059,7 @@ int gsi_kv_attention(const gsi_kv_cache* cache, const void* Q, int64_t T, int64_
   if (width < 1 || width > (1ll << 30) / cache->page) return fail(GSI_ERR_SHAPE, "%s: need width >= 1 and width * page <= 2^30, got %lld", fn, (long long)width);
   if (q_start == nullptr && B != T) return fail(GSI_ERR_SHAPE, "%s: without q_start every token is a request's only one: T = %lld, B = %lld", fn, (long long)T, (long long)B);
   if (T > 1 && q_stride < heads * a.c.dim) return fail(GSI_ERR_SHAPE, "%s: q_stride of %lld elements is less than a row of %lld", fn, (long long)q_stride, (long long)(heads * a.c.dim));
-  if (!(scale > -3.0e38f && scale < 3.0e38f)) return fail(GSI_ERR_SHAPE, "%s: scale is not a finite number", fn);
+  if (!(scale > -2.3e38f && scale < 2.3e38f)) return fail(GSI_ERR_SHAPE, "%s: scale * log2(e) is not a finite number", fn);
   GSI_REQUIRE_ALIGNED(Q, gsi::elem_size(dtype));
   GSI_REQUIRE_ALIGNED(O, 16);
   GSI_REQUIRE_ALIGNED(lse, 4);

@@ -28,8 +28,9 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kSlack = 8.f;
 
 // A score's factor in the exponential, above 0: the largest score is then the largest product, whose factor enters one fused operation with the
-// maximum's subtraction.  A negative scale turns the queries' sign; one of 0 becomes a number that changes no score.
-__device__ __forceinline__ float exponent_scale(float scale) { return fmaxf(fabsf(scale) * kLog2e, 1.17549435e-38f); }
+// maximum's subtraction.  A negative scale turns the queries' sign; one of 0 becomes the smallest number, 2^-149, which takes the largest products to
+// 2^-21 at most.
+__device__ __forceinline__ float exponent_scale(float scale) { return fmaxf(fabsf(scale) * kLog2e, 1.40129846e-45f); }
 
 struct Span {  // a request's tokens of the call and its keys
   int t0, n;
