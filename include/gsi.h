@@ -375,10 +375,12 @@ int gsi_kv_expand(const gsi_kv_cache* cache, const int32_t* slots, int64_t T, vo
  * h / (heads / cache->heads).  O[T, heads, dim] in `dtype`, 16-byte aligned.  A token that sees no key has O = 0, lse = -inf,
  * and so have tokens in front of q_start[0] and from q_start[B] on (q_start does not decrease).  Keys whose table entry names no page of the cache, or that lie past the request's row of the
  * table, are not seen; the others keep their numbers.  q_start NULL: every request has one token, B == T.
- * max_q, max_len: the most new tokens and keys that a request is expected to have.  They choose kernels and their launches; other
- * numbers cost time and never change what is computed.
- * Arithmetic: fp32 sums and statistics of bf16 products; keys and values are exact in bf16, queries and weights exp(s - max) enter in
- * one bf16 term (bf16: a query itself, a weight rounded once; for up to four rows in two terms) or in three (fp32; what a query has below
+ * max_q, max_len: the most new tokens and keys that a request is expected to have.  They choose kernels, tiles and launches: with
+ * any numbers every token has its attention over the same keys, in the arithmetic below.  Others than the true ones cost time, change the order
+ * of sums, and max_q the number of terms of bf16 weights.
+ * Arithmetic: fp32 sums and statistics of bf16 products; keys and values are exact in bf16.  bf16: a query is one term, a weight
+ * exp(s - max) is rounded once, to 2^-8 of itself; but where min(max_q, T) * heads / cache->heads <= 4 it has two terms, and an output is
+ * off by its own rounding alone (0.0017 of it in the mean, with one term up to 0.0025).  fp32: queries and weights have three terms (what a query has below
  * 2^-133 is lost, which counts where scale is 2^90 and more).  |scale| < 2.3e38: scale * log2(e) is a number too.
  * O may be Q itself (the same address, q_stride of a row); else O, lse and ws lie apart from each other and the inputs (refused).
  * ws: gsi_kv_attention_workspace_bytes(). */

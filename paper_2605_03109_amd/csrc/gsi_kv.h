@@ -36,7 +36,7 @@ struct KvAttend {
   int64_t B;
   const int32_t* table;
   int64_t width;
-  int64_t max_q, max_len;           // what the caller expects: they choose kernels and launches, never results
+  int64_t max_q, max_len;           // what the caller expects: they choose kernels, tiles and launches, never which keys are seen
   float scale;
   void* O;
   float* lse;                       // NULL: not written

@@ -637,7 +637,8 @@ def kv_attention(cache: KvCache, Q: torch.Tensor, q_start: Optional[torch.Tensor
                  ws=None, stream=None):
     """Attention of Q[T, heads, dim] (fp32 or bf16; tokens may lie further apart than a row) over the cache: O[T, heads, dim], or
     (O, lse[T, heads]) where ``lse`` is True or a tensor.  q_start None: one token a request.  max_q, max_len: what the
-    requests are expected to have at most (default: what the shapes allow); scale: 1 / sqrt(dim) by default."""
+    requests are expected to have at most (default: what the shapes allow, T where q_start is given).  They choose kernels, so a decode step with
+    q_start should say max_q=1; with max_q * heads / kv_heads <= 4 bf16 weights have two terms, else one.  scale: 1 / sqrt(dim) by default."""
     T, heads, dim = Q.shape
     B = kv_len.numel()
     if dim != cache.dim:
