@@ -51,7 +51,16 @@ __device__ __forceinline__ Span span_of(const KvAttend& a, int b) {
   return s;
 }
 
+// Codes as pairs of bf16, exact: pair SEL of a word, and its four.
 __device__ __forceinline__ float scale_value(int byte) { return __uint_as_float((uint32_t)byte << 23); }
+template <int SEL>
+__device__ __forceinline__ uint32_t two_values(uint32_t w, float scale) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, SEL));
+}
+__device__ __forceinline__ u32x4 eight_values(uint32_t w, float scale) {
+  return u32x4{two_values<0>(w, scale), two_values<1>(w, scale), two_values<2>(w, scale), two_values<3>(w, scale)};
+}
+
 __device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {  // both at least 0; the quotient of 64 bits takes a hundred instructions
   return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
 }

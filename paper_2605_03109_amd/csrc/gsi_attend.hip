@@ -77,14 +77,6 @@ __device__ __forceinline__ uint32_t word_of(const typename VWord<DPL>::type& v, 
   else return v;
 }
 
-template <int SEL>
-__device__ __forceinline__ uint32_t two_values(uint32_t w, float scale) {
-  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, SEL));
-}
-__device__ __forceinline__ bf16x8 eight_values(uint32_t w, float scale) {
-  return __builtin_bit_cast(bf16x8, u32x4{two_values<0>(w, scale), two_values<1>(w, scale), two_values<2>(w, scale), two_values<3>(w, scale)});
-}
-
 // Lane (c, g) of a wave: of a key, the 8 KW elements from 8 KW g on, of token 4 c + j; of a value, the DPL elements from DPL c on, of the tokens 16 g ..
 template <int DPL>
 struct Lane {
@@ -394,7 +386,7 @@ __global__ __launch_bounds__(kThreads, few_resident(sizeof(typename X::storage) 
         for (int w = 0; w < KW; ++w) {
           const int x = w / 4 < KB ? w / 4 : 0;
           const float sc = L.kin[x] ? scale_value((K.scale[x] >> (8 * j)) & 255u) : 1.f;
-          const bf16x8 k = eight_values(K.w[j][w], sc);
+          const bf16x8 k = __builtin_bit_cast(bf16x8, eight_values(K.w[j][w], sc));
 #pragma unroll
           for (int t = 0; t < CH; ++t) s[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[w][t], k, s[j], 0, 0, 0);
         }

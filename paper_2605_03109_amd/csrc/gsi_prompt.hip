@@ -83,13 +83,6 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
   const bf16x2 v = {(__bf16)a, (__bf16)b};
   return __builtin_bit_cast(uint32_t, v);
 }
-template <int SEL>
-__device__ __forceinline__ uint32_t two_values(uint32_t w, float scale) {
-  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, SEL));
-}
-__device__ __forceinline__ u32x4 eight_values(uint32_t w, float scale) {
-  return u32x4{two_values<0>(w, scale), two_values<1>(w, scale), two_values<2>(w, scale), two_values<3>(w, scale)};
-}
 
 // A lane's elements of a row of the output: 32 d + 8 i + 4 h .. of its ND blocks from block d0 on.
 template <class X, int ND>
