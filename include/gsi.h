@@ -372,7 +372,7 @@ int gsi_kv_expand(const gsi_kv_cache* cache, const int32_t* slots, int64_t T, vo
  * table[b, :], tokens q_start[b] .. q_start[b + 1] of which token i sees the keys j <= kv_len[b] - n + i (n tokens):
  *   s_j = scale * q . k_j,   O[t, h] = sum_j softmax(s)_j v_j,   lse[t, h] = log sum_j exp(s_j)  (natural; NULL: not written).
  * Q in `dtype`, token t at Q + t * q_stride elements, heads one after another; head h reads the keys of head
- * h / (heads / cache->heads).  O[T, heads, dim] in `dtype`, 16-byte aligned.  A token that sees no key has O = 0, lse = -inf,
+ * h / (heads / cache->heads).  O[T, heads, dim] in `dtype`, 16-byte aligned.  A token that sees no key, or whose scores are all -inf, has O = 0, lse = -inf,
  * and so have tokens in front of q_start[0] and from q_start[B] on (q_start does not decrease).  Keys whose table entry names no page of the cache, or that lie past the request's row of the
  * table, are not seen; the others keep their numbers.  q_start NULL: every request has one token, B == T.
  * max_q, max_len: the most new tokens and keys that a request is expected to have.  They choose kernels, tiles and launches: with
