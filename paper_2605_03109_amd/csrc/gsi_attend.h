@@ -231,22 +231,20 @@ __device__ __forceinline__ float row16_sum(float v) {
   return v + dpp_move<0x140>(v);
 }
 
-// Rows of tokens that belong to no request: zero.
+// Rows of tokens that belong to no request, in front of the first one's and behind the last one's: zero.
 template <class X>
 __device__ __forceinline__ void clear_idle_rows(const KvAttend& a) {
   if (!a.q_start) return;
-  // in front of the first request's, and behind the last one's
-  const int64_t first = a.B > 0 ? min(max(a.q_start[0], 0), (int)a.T) : 0;
-  const int64_t t0 = a.B > 0 ? min(max(a.q_start[a.B], (int)first), (int)a.T) : 0;
+  const int T = (int)a.T;
+  const int front = a.B > 0 ? min(max(a.q_start[0], 0), T) : 0, back = a.B > 0 ? min(max(a.q_start[a.B], front), T) : 0;
+  if (front == 0 && back == T) return;
   typename X::storage* const O = reinterpret_cast<typename X::storage*>(a.O);
   const int64_t row = (int64_t)a.heads * a.c.dim, all = (int64_t)gridDim.x * gridDim.y * blockDim.x;
   const int64_t me = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * blockDim.x + threadIdx.x;
-  for (int64_t i = t0 * row + me; i < a.T * row; i += all) X::store(O, i, 0.f);
-  for (int64_t i = me; i < first * row; i += all) X::store(O, i, 0.f);
-  if (a.lse) {
-    for (int64_t i = t0 * a.heads + me; i < a.T * a.heads; i += all) a.lse[i] = -INFINITY;
-    for (int64_t i = me; i < first * a.heads; i += all) a.lse[i] = -INFINITY;
-  }
+  const int64_t idle = front + (T - back), skip = back - front;
+  for (int64_t i = me; i < idle * row; i += all) X::store(O, i < front * row ? i : i + skip * row, 0.f);
+  if (a.lse)
+    for (int64_t i = me; i < idle * a.heads; i += all) a.lse[i < (int64_t)front * a.heads ? i : i + skip * a.heads] = -INFINITY;
 }
 
 // A rare path that is to stay a branch: the compiler would compute both sides for every element.  The condition is the same in every lane.
