@@ -326,7 +326,8 @@ size_t gsi_dense_stack_workspace_bytes(const gsi_map_desc* maps, int32_t n_maps,
  * page_id * page + offset.  A row (a token's 32 consecutive elements along a head) is held as E2M1 codes (1 sign, 2 exponent
  * bits, 1 mantissa bit: 0 .5 1 1.5 2 3 4 6) with one scale 2^(byte - 127): the smallest power of two with
  * max|x| / 2^e <= 6, byte 2 .. 254; codes are the nearest to x / 2^e, ties to the even code.  Byte 255 marks a block that
- * had an element that is not finite: all its values are NaN.  Codes lie two to a byte, the even element in the low half.
+ * had an element that is not finite: all its values are NaN.  (Elements from 3.5 * 2^126 = 2.98e38 on stand for 2^128, which is infinite
+ * in fp32 and bf16.)  Codes lie two to a byte, the even element in the low half.
  * Limits: dim a multiple of 32 up to 256, page a power of two in 16 .. 4096, n_pages * page < 2^31. */
 typedef struct gsi_kv_cache {
   uint8_t* K;         /* device, [n_pages, heads, page, dim / 2] codes of the keys, 16-byte aligned like the rest   */

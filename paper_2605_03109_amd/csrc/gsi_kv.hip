@@ -1,8 +1,8 @@
 // The paged cache of keys and values in 4 bits: its tables, its rows written and read back.
 //
 // E2M1: sign, then 0 .5 1 1.5 2 3 4 6.  Of 32 elements along a head the scale is the smallest 2^e (byte e + 127, in
-// 2 .. 254) with max|x| / 2^e <= 6, so that nothing saturates and every value is a normal number or zero; an element's code
-// is the nearest to x / 2^e, ties to the even code (the division is exact).  A block with an element that is not
+// 2 .. 254) with max|x| / 2^e <= 6, so that nothing saturates and every value is a normal number or zero (but those of elements from 3.5 * 2^126 on,
+// which round to 2^128: infinite); an element's code is the nearest to x / 2^e, ties to the even code (the division is exact).  A block with an element that is not
 // finite gets the byte 255: every value of it reads as NaN.  The conversions are the card's own (the formats of its
 // matrix instructions); they round as written here for every scale.
 #include <algorithm>
