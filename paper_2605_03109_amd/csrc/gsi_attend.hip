@@ -8,10 +8,10 @@
 // once with zeros against the odd elements and once with zeros against the even ones, as two rows of the product.
 //
 // Memory bounds it where contexts are long: every code and scale is read once, by eight waves a unit that request a step's keys and values while they
-// work on the step before.  8 contexts of 131000 keys x 8 heads x 128 are read at 5.3 TB/s, two of 60000 and 131000 (208 MB) at 4.5 in 46 us, 64
-// fp32 tokens x 32 heads over 287 MB at 4.4 in 65 us (a copy moves 4.9 TB/s); 5 to 8 us of join_kernel come on top.  In those the matrix units are busy
+// work on the step before.  8 contexts of 131000 keys x 8 heads x 128 are read at 5.3 TB/s, two of 60000 and 131000 (208 MB) at 4.6 in 45.5 us, 64
+// fp32 tokens x 32 heads over 287 MB at 4.4 in 64 us (streaming reads reach 6.5 TB/s); 5 to 8 us of join_kernel come on top.  In those the matrix units are busy
 // for 11 % of the time, and the conversions of codes, exponentials and sums take about half of the issue slots of a SIMD's two waves.  Short
-// contexts are bound by the chain of loads in front of the first product: one token of 12 heads over 210 keys 8.2 us.
+// contexts are bound by the chain of loads in front of the first product: one token of 12 heads over 210 keys 8.4 us.
 #include <algorithm>
 
 #include "gsi_attend.h"

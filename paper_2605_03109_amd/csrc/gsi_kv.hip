@@ -54,7 +54,7 @@ __device__ __forceinline__ int owner(const int* start, int n, int x) {
 
 // Every workgroup scans the lengths of all requests (they are few bytes, and a second launch would cost more than the
 // scan) and then takes its share of the tokens, the new pages and the requests.  Latency bounds it: lengths, scans in LDS, a search, one
-// read of the table or the free list.  32 requests 4.4 us, 300 requests of 27000 new tokens 5.5 us.
+// read of the table or the free list.  32 requests 4.5 us, 300 requests of 27000 new tokens 6.0 us.
 __global__ __launch_bounds__(kScanThreads) void tables_kernel(const int32_t* __restrict__ kv_len, const int32_t* __restrict__ n_new, int B,
                                                               const int32_t* __restrict__ free_pages,
                                                               const int32_t* __restrict__ n_free, int free_cap,
@@ -131,7 +131,7 @@ __global__ __launch_bounds__(kScanThreads) void tables_kernel(const int32_t* __r
 // ---- rows ------------------------------------------------------------------------------------------------
 // A workgroup takes 16 tokens by 128 elements, 8 elements a thread: four threads hold the block of a scale, and the scale bytes of
 // consecutive tokens, which lie side by side, come from one workgroup.  Memory bounds both directions: 8192 tokens x 32 heads x 128 in bf16, 170 MB,
-// are written in 35 us (4.9 TB/s) and read back in 26 us (6.5 TB/s); 8 tokens x 12 x 64 take 2.9 us each.
+// are written in 34 us (5.0 TB/s, a copy's rate) and read back in 26 us (6.5 TB/s); 8 tokens x 12 x 64 take 2.9 us each.
 constexpr int kRowTokens = 16, kRowThreads = 256, kRowElems = 128;
 
 struct RowPlace {

@@ -6,10 +6,10 @@
 // contraction taken in the order of the accumulator's registers).  Keys and values are converted once, on their way to LDS; values are read
 // there with the transposing reads.  (By each wave for itself, chunks of 512 tokens behind 6000 to 15000 keys took 410 us; this way 379.)
 //
-// Issue bounds it: those chunks, 346 GFLOP, run at 0.91 PFLOP/s (a library product of 8192^3 at 1.2), with the matrix units busy for a third of the time;
+// Issue bounds it: those chunks, 346 GFLOP, run at 0.92 PFLOP/s (a plain loop of matrix instructions on random data at 1.47), with the matrix units busy for a third of the time;
 // exponentials, sums, the conversion of the next step and the reads of LDS take the slots of a SIMD's two waves beside them.  2048 tokens from the
 // first on x 32 heads x 128, 34 GFLOP, take 58 us: tiles of one round, of which the longest, alone on its unit towards the end, sets the time.
-// fp32 rows have three products in place of one: six prompts of 90 to 700 tokens, 24 heads over 8 of 96, 33 GFLOP as bf16, 62 us.
+// fp32 rows have three products in place of one: six prompts of 90 to 700 tokens, 24 heads over 8 of 96, 33 GFLOP as bf16, 61 us.
 #include <algorithm>
 
 #include "gsi_attend.h"
