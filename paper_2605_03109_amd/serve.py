@@ -25,6 +25,8 @@ class AttentionBlock:
     the cache, and `missing` says so: it is the number of pages that were not there, summed over the steps (on the device, 0 where nothing was lost;
     a step whose `status[1]` is not 0 has lost tokens, and its requests are to be dropped or given again)."""
 
+    KEPT = 8  # step sizes whose buffers are kept, in order of use
+
     def __init__(self, weights: Dict[str, torch.Tensor], U_in: torch.Tensor, U_out: torch.Tensor, heads: int, kv_heads: int,
                  requests: int, n_pages: int, max_len: int, page: int = 64, eps: float = 0.05):
         dev = U_in.device
@@ -48,11 +50,13 @@ class AttentionBlock:
     def n_free(self) -> torch.Tensor:
         return self._count[:1]
 
+    @n_free.setter
+    def n_free(self, n: torch.Tensor) -> None:
+        self._count = torch.cat([n.view(1), self._count[1:]])
+
     @property
     def missing(self) -> torch.Tensor:
         return self._count[1:]
-
-    KEPT = 8  # step sizes whose buffers are kept, in order of use
 
     def _stacks_for(self, T: int) -> tuple:
         # buffers by stream too: memory that one gives back is used again behind the work of its own stream only

@@ -34,6 +34,19 @@ def test_pages_that_run_out_are_reported():
     assert block.status.tolist() == [0, 1] and int(block.missing) == 2 and int(block.n_free) == 0
 
 
+def test_a_block_set_back():
+    """Lengths, free list and their count as they were: the same step again gives the same."""
+    block, step = block_of(n_pages=12, max_len=160)
+    step(30, 10)
+    state, table = (block.kv_len, block.free, block.n_free), block.table.clone()
+    X, n_new = torch.randn(21, 256, device="cuda"), torch.tensor([20, 1], dtype=torch.int32, device="cuda")
+    first = block.step(X, n_new, 20).clone()
+    block.kv_len, block.free, block.n_free = state
+    block.table.copy_(table)
+    assert torch.equal(block.step(X, n_new, 20), first)
+    assert int(block.n_free) == 12 - 4 - 1 and int(block.missing) == 0
+
+
 def test_requests_past_their_length_are_reported():
     block, step = block_of(n_pages=20, max_len=32)
     step(32, 5)
